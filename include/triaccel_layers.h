@@ -1,0 +1,215 @@
+/*
+ * triaccel_layers.h -- C ABI of the layer operators that stand beside the optimizer step: the feed-forward half of a
+ * block, forward and backward, in each of the three precisions that the step stores parameters in.
+ *
+ *   linear         y = r + s drop(act(x W^T + b))
+ *   gated          h = act(x Wg^T + bg) * (x Wu^T + bu)
+ *   residual_norm  r' = r + s g * P(b),  y = N(r')
+ *   dropout        y = r + s drop(x)
+ *
+ * The library is the optimizer step's (triaccel.h): the same dtype codes, return codes and triaccel_last_error.
+ * Every function is asynchronous on `hip_stream` (a hipStream_t, NULL = the default stream) and uses the current device;
+ * none allocates, synchronises or keeps anything between calls, so all of them can be captured into a HIP graph.  What a
+ * call needs beside its operands is a workspace of the caller's, of the size that the function's _workspace companion
+ * gives for the same arguments (pointers are not read by it); it may be used again as soon as the call is done on the
+ * stream.  The workspace is 16-byte aligned; every other pointer needs the alignment of its element only.
+ *
+ * Matrices are row-major with unit column stride; `ld*` is the distance of rows in elements, at least the row's length.
+ * Sizes: 1 <= in, out < 2^31, 0 <= rows < 2^31 (no rows: a forward call does nothing, gradients of weights are zero).
+ * An output may be the same matrix as the residual it is added to; apart from that outputs overlap neither inputs nor
+ * each other.  x, W and all matrices of a call have its `dtype`; vectors (biases, norm weights, gates) have a code of
+ * their own, since the step may store a layer's vectors in another precision than the layer computes in.
+ *
+ * Arithmetic: products are summed in fp32, in an order that depends on the sizes, strides and alignment alone: the same
+ * call gives the same bits.  FP32 operands are split into three BF16 parts each and the six largest partial products
+ * kept (a relative error of 2^-24 per product, as in an fp32 multiplication); where an operand is not finite the outputs
+ * that it enters are not finite either, but may be NaN where one fp32 product would be infinite.
+ *
+ * drop(v)_i = v_i / q for kept elements and 0 for others, q = 1 - t / 65536, t = min(65535, round(65536 p)).  Element i of
+ * the dense (rows, columns) matrix, i = row * columns + column, is dropped if half-word i % 8 (low halves first) of
+ * Philox4x32 with 7 rounds (Salmon et al., 2011) is below t; counter = (i / 8, offset) as two 64-bit words, key = seed.
+ * The mask is computed again wherever it is needed and never stored.
+ */
+#ifndef TRIACCEL_LAYERS_H
+#define TRIACCEL_LAYERS_H
+
+#include <stdint.h>
+
+#include "triaccel.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define TRIACCEL_ACT_NONE 0
+#define TRIACCEL_ACT_RELU 1
+#define TRIACCEL_ACT_SILU 2      /* z / (1 + exp(-z))                                        */
+#define TRIACCEL_ACT_GELU 3      /* z Phi(z), Phi the normal distribution function            */
+#define TRIACCEL_ACT_GELU_TANH 4 /* z / (1 + exp(-2 sqrt(2 / pi) (z + 0.044715 z^3)))         */
+
+#define TRIACCEL_NORM_NONE 0
+#define TRIACCEL_NORM_RMS 1   /* v / sqrt(mean(v^2) + eps) * weight + bias                   */
+#define TRIACCEL_NORM_LAYER 2 /* (v - mean(v)) / sqrt(var(v) + eps) * weight + bias          */
+
+#define TRIACCEL_NORM_MAX_COLS 16384
+
+/* p = 0: no dropout.  device_seed (device, two words: seed, offset) takes the place of the two values if it is not NULL,
+   so that a captured graph can get another mask at each replay. */
+typedef struct {
+  double p; /* in [0, 1) */
+  uint64_t seed, offset;
+  const uint64_t *device_seed;
+} triaccel_dropout_spec;
+
+typedef struct {
+  uint32_t struct_size; /* sizeof(triaccel_linear_args) */
+  int32_t dtype;
+  int64_t rows, in, out;
+  const void *x;      int64_t ldx;    /* rows x in                                              */
+  const void *weight; int64_t ldw;    /* out x in                                               */
+  const void *bias;                   /* out values of bias_dtype, or NULL                      */
+  const void *residual; int64_t ldr;  /* rows x out, or NULL                                    */
+  void *y;   int64_t ldy;             /* rows x out                                             */
+  void *pre; int64_t ldpre;           /* rows x out: x W^T + b, kept for the backward; or NULL  */
+  int32_t bias_dtype, act;
+  float scale;
+  int32_t reserved_;                  /* 0 */
+  triaccel_dropout_spec drop;
+  void *workspace; uint64_t workspace_bytes;
+} triaccel_linear_args;
+
+int64_t triaccel_linear_workspace(const triaccel_linear_args *args);
+int triaccel_linear(const triaccel_linear_args *args, void *hip_stream);
+
+/* dz = s drop(dy) act'(pre), dx = dz W, dW = dz^T x, db = sum over the rows of dz; the gradient of the residual is dy. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(triaccel_linear_backward_args) */
+  int32_t dtype;
+  int64_t rows, in, out;
+  const void *dy;     int64_t lddy;   /* rows x out                                             */
+  const void *x;      int64_t ldx;    /* rows x in; read for dweight                            */
+  const void *weight; int64_t ldw;    /* out x in; read for dx                                  */
+  const void *pre;    int64_t ldpre;  /* rows x out; read unless act is NONE                    */
+  void *dx;      int64_t lddx;        /* rows x in, or NULL                                     */
+  void *dweight; int64_t lddw;        /* out x in, dense or not, or NULL                        */
+  void *dbias;                        /* out values of dbias_dtype, or NULL                     */
+  int32_t dweight_dtype;              /* the call's dtype, or FP32                              */
+  int32_t dbias_dtype, act;
+  float scale;
+  triaccel_dropout_spec drop;
+  void *workspace; uint64_t workspace_bytes;
+} triaccel_linear_backward_args;
+
+int64_t triaccel_linear_backward_workspace(const triaccel_linear_backward_args *args);
+int triaccel_linear_backward(const triaccel_linear_backward_args *args, void *hip_stream);
+
+typedef struct {
+  uint32_t struct_size; /* sizeof(triaccel_gated_args) */
+  int32_t dtype;
+  int64_t rows, in, out;
+  const void *x; int64_t ldx;                  /* rows x in                                     */
+  const void *w_gate; const void *w_up; int64_t ldw; /* out x in each                           */
+  const void *b_gate; const void *b_up;        /* out values of bias_dtype each, or both NULL   */
+  void *h; int64_t ldh;                        /* rows x out                                    */
+  void *gate; void *up; int64_t ldg;           /* rows x out each, kept for the backward, or both NULL */
+  int32_t bias_dtype, act;
+  void *workspace; uint64_t workspace_bytes;
+} triaccel_gated_args;
+
+int64_t triaccel_gated_workspace(const triaccel_gated_args *args);
+int triaccel_gated(const triaccel_gated_args *args, void *hip_stream);
+
+/* dg = dh up act'(gate), du = dh act(gate); dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x, db = sums over the rows. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(triaccel_gated_backward_args) */
+  int32_t dtype;
+  int64_t rows, in, out;
+  const void *dh; int64_t lddh;                /* rows x out                                    */
+  const void *x;  int64_t ldx;                 /* rows x in; read for the weights' gradients    */
+  const void *w_gate; const void *w_up; int64_t ldw; /* out x in each; read for dx              */
+  const void *gate; const void *up; int64_t ldg;     /* rows x out each                         */
+  void *dx; int64_t lddx;                      /* rows x in, or NULL                            */
+  void *dw_gate; void *dw_up; int64_t lddw;    /* out x in each, or both NULL                   */
+  void *db_gate; void *db_up;                  /* out values of dbias_dtype each, or both NULL  */
+  int32_t dweight_dtype;                       /* the call's dtype, or FP32                     */
+  int32_t dbias_dtype, act;
+  int32_t reserved_;                           /* 0 */
+  void *workspace; uint64_t workspace_bytes;
+} triaccel_gated_backward_args;
+
+int64_t triaccel_gated_backward_workspace(const triaccel_gated_backward_args *args);
+int triaccel_gated_backward(const triaccel_gated_backward_args *args, void *hip_stream);
+
+typedef struct {
+  int32_t kind;  /* TRIACCEL_NORM_* */
+  int32_t dtype; /* of weight and bias */
+  const void *weight, *bias; /* cols values each; NULL = ones, zeros */
+  float eps;     /* > 0 */
+  int32_t reserved_; /* 0 */
+} triaccel_norm_spec;
+
+/* r' = r + s g * P(b), y = N(r').  1 <= cols <= TRIACCEL_NORM_MAX_COLS.  block NULL: r' is the residual and is not
+   written.  norm.kind NONE: y is not written.  r' enters N before it is rounded to `dtype`. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(triaccel_residual_norm_args) */
+  int32_t dtype;
+  int64_t rows, cols;
+  const void *residual; int64_t ldr;
+  const void *block;    int64_t ldb;           /* or NULL                                       */
+  const void *gate;     int64_t ldgate;        /* values of gate_dtype: row i / rows_per_gate is multiplied to row i of the
+                                                  block; NULL = ones                            */
+  int64_t rows_per_gate;                       /* 0: one row of gates for all                   */
+  void *residual_out; int64_t ldro;
+  void *y; int64_t ldy;
+  int32_t gate_dtype;
+  float scale;
+  triaccel_norm_spec post, norm;               /* P and N                                       */
+} triaccel_residual_norm_args;
+
+int triaccel_residual_norm(const triaccel_residual_norm_args *args, void *hip_stream);
+
+/* From dresidual_out (NULL = 0) and dy (NULL = 0; read unless norm.kind is NONE), with `residual` the r' that the forward
+   wrote (r if it had no block): dresidual = the gradient of r, dblock of b, and the gradients of the gate and of the
+   norms' weights and biases, each of `dvec_dtype`, where the pointer is not NULL.  dgate has the gate's rows, dense. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(triaccel_residual_norm_backward_args) */
+  int32_t dtype;
+  int64_t rows, cols;
+  const void *dresidual_out; int64_t lddro;
+  const void *dy;            int64_t lddy;
+  const void *residual;      int64_t ldr;
+  const void *block;         int64_t ldb;
+  const void *gate;          int64_t ldgate;
+  int64_t rows_per_gate;
+  void *dresidual; int64_t lddr;
+  void *dblock;    int64_t lddb;
+  void *dgate, *dpost_weight, *dpost_bias, *dnorm_weight, *dnorm_bias;
+  int32_t gate_dtype, dvec_dtype;
+  float scale;
+  int32_t reserved_;                           /* 0 */
+  triaccel_norm_spec post, norm;
+  void *workspace; uint64_t workspace_bytes;
+} triaccel_residual_norm_backward_args;
+
+int64_t triaccel_residual_norm_backward_workspace(const triaccel_residual_norm_backward_args *args);
+int triaccel_residual_norm_backward(const triaccel_residual_norm_backward_args *args, void *hip_stream);
+
+/* y = r + s drop(x).  The gradient of x is the same call on the gradient of y, without a residual. */
+typedef struct {
+  uint32_t struct_size; /* sizeof(triaccel_dropout_args) */
+  int32_t dtype;
+  int64_t rows, cols;
+  const void *x; int64_t ldx;
+  const void *residual; int64_t ldr;           /* or NULL                                       */
+  void *y; int64_t ldy;
+  float scale;
+  int32_t reserved_;                           /* 0 */
+  triaccel_dropout_spec drop;
+} triaccel_dropout_args;
+
+int triaccel_dropout(const triaccel_dropout_args *args, void *hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* TRIACCEL_LAYERS_H */

@@ -1,5 +1,6 @@
 """MI355X-native Tri-Accel optimizer step (arXiv 2508.16905): hand-written gfx950 kernels behind
-a C ABI (``include/triaccel.h``), with a ctypes binding of the same names.
+a C ABI (``include/triaccel.h``), with a ctypes binding of the same names; and beside it the layer operators
+of a feed-forward block (``include/triaccel_layers.h``) on torch tensors.
 
 Importing this package loads nothing; the HIP library is loaded on first use and its absence is
 an error (there is no CPU path in the product).
@@ -36,5 +37,17 @@ from .binding import (  # noqa: F401
     triaccel_stage_times_get,
     triaccel_step,
     triaccel_strerror,
+)
+from .layers import (  # noqa: F401
+    Dropout,
+    Norm,
+    dropout,
+    dropout_backward,
+    gated,
+    gated_backward,
+    linear,
+    linear_backward,
+    residual_norm,
+    residual_norm_backward,
 )
 from .optimizer import TriAccel  # noqa: F401

@@ -161,6 +161,101 @@ EXPORTS = {
                                              C.c_void_p, C.c_void_p]),
 }
 
+
+# ---- the layer operators of include/triaccel_layers.h -------------------------------------------
+
+class DropoutSpec(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64), ("device_seed", C.c_void_p)]
+
+
+class LinearArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64),
+        ("x", C.c_void_p), ("ldx", C.c_int64), ("weight", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
+        ("residual", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64), ("pre", C.c_void_p), ("ldpre", C.c_int64),
+        ("bias_dtype", C.c_int32), ("act", C.c_int32), ("scale", C.c_float), ("reserved_", C.c_int32), ("drop", DropoutSpec),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+
+class LinearBackwardArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64),
+        ("dy", C.c_void_p), ("lddy", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64), ("weight", C.c_void_p), ("ldw", C.c_int64),
+        ("pre", C.c_void_p), ("ldpre", C.c_int64), ("dx", C.c_void_p), ("lddx", C.c_int64), ("dweight", C.c_void_p), ("lddw", C.c_int64),
+        ("dbias", C.c_void_p), ("dweight_dtype", C.c_int32), ("dbias_dtype", C.c_int32), ("act", C.c_int32), ("scale", C.c_float),
+        ("drop", DropoutSpec), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+
+class GatedArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64),
+        ("x", C.c_void_p), ("ldx", C.c_int64), ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("ldw", C.c_int64),
+        ("b_gate", C.c_void_p), ("b_up", C.c_void_p), ("h", C.c_void_p), ("ldh", C.c_int64),
+        ("gate", C.c_void_p), ("up", C.c_void_p), ("ldg", C.c_int64), ("bias_dtype", C.c_int32), ("act", C.c_int32),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+
+class GatedBackwardArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("rows", C.c_int64), ("in_", C.c_int64), ("out", C.c_int64),
+        ("dh", C.c_void_p), ("lddh", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
+        ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("ldw", C.c_int64), ("gate", C.c_void_p), ("up", C.c_void_p), ("ldg", C.c_int64),
+        ("dx", C.c_void_p), ("lddx", C.c_int64), ("dw_gate", C.c_void_p), ("dw_up", C.c_void_p), ("lddw", C.c_int64),
+        ("db_gate", C.c_void_p), ("db_up", C.c_void_p), ("dweight_dtype", C.c_int32), ("dbias_dtype", C.c_int32), ("act", C.c_int32),
+        ("reserved_", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+
+class NormSpec(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("dtype", C.c_int32), ("weight", C.c_void_p), ("bias", C.c_void_p), ("eps", C.c_float),
+                ("reserved_", C.c_int32)]
+
+
+class ResidualNormArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+        ("residual", C.c_void_p), ("ldr", C.c_int64), ("block", C.c_void_p), ("ldb", C.c_int64), ("gate", C.c_void_p), ("ldgate", C.c_int64),
+        ("rows_per_gate", C.c_int64), ("residual_out", C.c_void_p), ("ldro", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64),
+        ("gate_dtype", C.c_int32), ("scale", C.c_float), ("post", NormSpec), ("norm", NormSpec),
+    ]
+
+
+class ResidualNormBackwardArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+        ("dresidual_out", C.c_void_p), ("lddro", C.c_int64), ("dy", C.c_void_p), ("lddy", C.c_int64), ("residual", C.c_void_p), ("ldr", C.c_int64),
+        ("block", C.c_void_p), ("ldb", C.c_int64), ("gate", C.c_void_p), ("ldgate", C.c_int64), ("rows_per_gate", C.c_int64),
+        ("dresidual", C.c_void_p), ("lddr", C.c_int64), ("dblock", C.c_void_p), ("lddb", C.c_int64),
+        ("dgate", C.c_void_p), ("dpost_weight", C.c_void_p), ("dpost_bias", C.c_void_p), ("dnorm_weight", C.c_void_p),
+        ("dnorm_bias", C.c_void_p), ("gate_dtype", C.c_int32), ("dvec_dtype", C.c_int32), ("scale", C.c_float), ("reserved_", C.c_int32),
+        ("post", NormSpec), ("norm", NormSpec), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+    ]
+
+
+class DropoutArgs(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+        ("x", C.c_void_p), ("ldx", C.c_int64), ("residual", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64),
+        ("scale", C.c_float), ("reserved_", C.c_int32), ("drop", DropoutSpec),
+    ]
+
+
+# A workspace query and a call per operator; the calls take the stream as well.
+_LAYER_CALLS = {
+    "triaccel_linear": (LinearArgs, True), "triaccel_linear_backward": (LinearBackwardArgs, True),
+    "triaccel_gated": (GatedArgs, True), "triaccel_gated_backward": (GatedBackwardArgs, True),
+    "triaccel_residual_norm": (ResidualNormArgs, False), "triaccel_residual_norm_backward": (ResidualNormBackwardArgs, True),
+    "triaccel_dropout": (DropoutArgs, False),
+}
+LAYER_EXPORTS = {}
+for _name, (_args, _workspace) in _LAYER_CALLS.items():
+    LAYER_EXPORTS[_name] = (C.c_int, [C.POINTER(_args), C.c_void_p])
+    if _workspace:
+        LAYER_EXPORTS[_name + "_workspace"] = (C.c_int64, [C.POINTER(_args)])
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -170,7 +265,7 @@ class TriAccelError(RuntimeError):
         detail = ""
         if _lib is not None:
             detail = _lib.triaccel_strerror(code).decode()
-            if code == -6 or (code == -1 and where == "triaccel_power_iter_static"):
+            if code == -6 or (code == -1 and where == "triaccel_power_iter_static") or where in LAYER_EXPORTS:
                 detail += " -- " + _lib.triaccel_last_error().decode()
         super().__init__(f"{where} failed with code {code}: {detail}")
 
@@ -186,7 +281,7 @@ def load_library() -> C.CDLL:
             "(python -m paper_2508_16905_amd.build, or __graft_entry__.build())"
         )
     lib = C.CDLL(LIB_PATH)
-    for name, (res, args) in EXPORTS.items():
+    for name, (res, args) in (*EXPORTS.items(), *LAYER_EXPORTS.items()):
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args

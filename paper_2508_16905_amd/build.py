@@ -9,7 +9,9 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtriaccel.so")
-SOURCES = ["kernels.hip", "update.hip", "update_local.hip", "update_resize.hip", "power.hip", "api.hip"]
+SOURCES = ["kernels.hip", "update.hip", "update_local.hip", "update_resize.hip", "power.hip", "api.hip",
+           "layers/gemm_fp16.hip", "layers/gemm_bf16.hip", "layers/gemm_fp32.hip", "layers/rowwise.hip", "layers/residual_norm.hip",
+           "layers/layers_api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
@@ -33,8 +35,8 @@ HIPCC_FLAGS = [
 
 def build_library(force: bool = True, verbose: bool = False) -> str:
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    deps = srcs + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    deps.append(os.path.join(os.path.dirname(HERE), "include", "triaccel.h"))
+    deps = srcs + [os.path.join(d, f) for d in (CSRC, os.path.join(CSRC, "layers"), os.path.join(os.path.dirname(HERE), "include"))
+                   for f in os.listdir(d) if f.endswith(".h")]
     if not force and os.path.exists(LIB) and all(os.path.getmtime(LIB) >= os.path.getmtime(d) for d in deps):
         return LIB
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

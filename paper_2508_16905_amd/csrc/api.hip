@@ -42,6 +42,17 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 }  // namespace
 
+namespace triaccel {
+// Text of a refusal or failure in another file of the library.  Without memory for it the last text is left out.
+void note_error(const char* text) noexcept {
+  try {
+    g_last_error = text;
+  } catch (...) {
+    g_last_error.clear();
+  }
+}
+}  // namespace triaccel
+
 struct StepGraph {
   hipGraph_t graph = nullptr;
   hipGraphExec_t exec = nullptr;

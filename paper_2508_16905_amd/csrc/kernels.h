@@ -7,6 +7,9 @@
 
 namespace triaccel {
 
+// Sets the text that triaccel_last_error returns (api.hip).
+void note_error(const char* text) noexcept;
+
 // A pointer into device memory that kernels read from memory themselves.  They have to know that it is a global one: of
 // any other they make FLAT accesses (numerics.h), with a 64-bit address per lane and never through the scalar caches.
 template <typename T>

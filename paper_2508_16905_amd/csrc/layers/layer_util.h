@@ -1,0 +1,207 @@
+// What the layer kernels share: groups of eight elements, activations, the dropout generator.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../numerics.h"
+
+namespace triaccel {
+namespace layers {
+
+enum Act : int { kNone = 0, kRelu = 1, kSilu = 2, kGelu = 3, kGeluTanh = 4 };
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+
+template <int DT> struct ElemOf { typedef __bf16 T; typedef bf16x8 V; };
+template <> struct ElemOf<kFP16> { typedef _Float16 T; typedef f16x8 V; };
+template <> struct ElemOf<kFP32> { typedef float T; typedef __attribute__((ext_vector_type(8))) float V; };
+template <int DT> using Elem = typename ElemOf<DT>::T;
+template <int DT> using Elem8 = typename ElemOf<DT>::V;
+
+// Eight elements as they lie in memory, at any element's alignment (gfx950 loads and stores vectors unaligned).
+template <int DT>
+__device__ __forceinline__ Elem8<DT> load_raw8(const Elem<DT>* p) {
+  typedef Elem8<DT> __attribute__((aligned(sizeof(Elem<DT>)))) U;
+  return *(const TA_GLOBAL U*)(p);
+}
+// The first `n` of them, zeros behind.
+template <int DT>
+__device__ __forceinline__ Elem8<DT> load_raw8(const Elem<DT>* p, int64_t n) {
+  if (n >= 8) return load_raw8<DT>(p);
+  Elem8<DT> v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = i < n ? *as_global<Elem<DT>>(p + i) : (Elem<DT>)0.0f;
+  return v;
+}
+template <int DT>
+__device__ __forceinline__ void load8(const void* base, int64_t at, int64_t n, float (&out)[8]) {
+  const Elem8<DT> v = load_raw8<DT>((const Elem<DT>*)base + at, n);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) out[i] = (float)v[i];
+}
+// A vector whose type is known at run time only; eight values of it.
+__device__ __forceinline__ void load8_of(int dtype, const void* base, int64_t at, int64_t n, float (&out)[8]) {
+  if (dtype == kFP32) load8<kFP32>(base, at, n, out);
+  else if (dtype == kBF16) load8<kBF16>(base, at, n, out);
+  else load8<kFP16>(base, at, n, out);
+}
+
+template <int DT>
+__device__ __forceinline__ Elem<DT> narrow(float v) {
+  if constexpr (DT == kFP32) return v;
+  asm volatile("" : "+v"(v));  // rounded to fp32 first, as numerics.h has it
+  return (Elem<DT>)v;
+}
+template <int DT>
+__device__ __forceinline__ void store8(void* base, int64_t at, int64_t n, const float (&in)[8]) {
+  Elem<DT>* p = (Elem<DT>*)base + at;
+  Elem8<DT> v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = narrow<DT>(in[i]);
+  if (n >= 8) {
+    typedef Elem8<DT> __attribute__((aligned(sizeof(Elem<DT>)))) U;
+    *(TA_GLOBAL U*)(p) = v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < n) *as_global<Elem<DT>>(p + i) = v[i];
+}
+__device__ __forceinline__ void store1_of(int dtype, void* base, int64_t at, float v) {
+  if (dtype == kFP32) as_global<float>(base)[at] = v;
+  else if (dtype == kBF16) as_global<__bf16>(base)[at] = narrow<kBF16>(v);
+  else as_global<_Float16>(base)[at] = narrow<kFP16>(v);
+}
+
+// ---- activations ------------------------------------------------------------------------------------------------
+// EXACT: for fp32 results.  Results of 16 bits take the hardware's exponential and reciprocal (each within 1 unit in the
+// last place of fp32, 2^-23: nothing beside their half step of 2^-9 or 2^-12).
+template <bool EXACT>
+__device__ __forceinline__ float logistic(float z) {
+  if constexpr (EXACT) return 1.0f / (1.0f + expf(-z));
+  else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z));
+}
+constexpr float kTanhA = 1.5957691216057308f;  // 2 sqrt(2 / pi): 1/2 (1 + tanh q) is the logistic function of 2 q
+constexpr float kTanhB = 0.044715f;
+// Phi(z).  erfc and not 1 + erf: for negative z the sum would cancel.
+__device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(-0.70710678118654752f * z); }
+
+template <bool EXACT>
+__device__ __forceinline__ float act_value(int act, float z) {
+  switch (act) {
+    case kRelu: return z <= 0.0f ? 0.0f : z;  // a NaN stays one
+    case kSilu: return z * logistic<EXACT>(z);
+    case kGelu: return z * normal_cdf(z);
+    case kGeluTanh: return z * logistic<EXACT>(kTanhA * fmaf(kTanhB * z * z, z, z));
+    default: return z;
+  }
+}
+// Past 32 the logistic function is 0 or 1 in fp32; held there, so that the cube cannot overflow in the slope.
+__device__ __forceinline__ float held(float z) { return fminf(fmaxf(z, -32.0f), 32.0f); }
+// act(z) and act'(z)
+template <bool EXACT>
+__device__ __forceinline__ void act_both(int act, float z, float& value, float& slope) {
+  switch (act) {
+    case kRelu:
+      value = z <= 0.0f ? 0.0f : z;
+      slope = z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
+      return;
+    case kSilu: {
+      const float t = logistic<EXACT>(z);
+      value = z * t;
+      slope = fmaf(value, 1.0f - t, t);
+      return;
+    }
+    case kGelu: {
+      const float c = normal_cdf(z);
+      value = z * c;
+      slope = fmaf(z * 0.3989422804014327f, expf(-0.5f * z * z), c);
+      return;
+    }
+    case kGeluTanh: {
+      const float h = held(z), t = logistic<EXACT>(kTanhA * fmaf(kTanhB * h * h, h, h));
+      value = z * t;
+      slope = fmaf(value * (1.0f - t), kTanhA * fmaf(3.0f * kTanhB * h, h, 1.0f), t);
+      return;
+    }
+    default: value = z; slope = 1.0f;
+  }
+}
+
+// ---- dropout ----------------------------------------------------------------------------------------------------
+struct Drop {
+  uint64_t seed, offset;
+  const uint64_t* device_seed;
+  uint32_t limit;  // a half-word below it drops its element; 0: no dropout
+  float factor;    // of what is kept: the call's scale, over the probability to be kept
+};
+struct DropKey {
+  uint32_t k0, k1, c2, c3;
+};
+__device__ __forceinline__ DropKey drop_key(const Drop& d) {
+  uint64_t seed = d.seed, offset = d.offset;
+  if (d.device_seed) {
+    seed = as_global<uint64_t>(d.device_seed)[0];
+    offset = as_global<uint64_t>(d.device_seed)[1];
+  }
+  return DropKey{(uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)offset, (uint32_t)(offset >> 32)};
+}
+// Philox4x32, 7 rounds: the fewest that its authors report to pass the whole of their test batteries.  A mask needs no
+// more, and a round costs four 32-bit multiplications of a quarter of the rate for each eight elements.
+__device__ __forceinline__ void philox7(const DropKey& key, uint64_t counter, uint32_t (&w)[4]) {
+  uint32_t k0 = key.k0, k1 = key.k1;
+  w[0] = (uint32_t)counter; w[1] = (uint32_t)(counter >> 32); w[2] = key.c2; w[3] = key.c3;
+#pragma unroll
+  for (int r = 0; r < 7; ++r) {
+    const uint64_t p0 = (uint64_t)0xD2511F53u * w[0], p1 = (uint64_t)0xCD9E8D57u * w[2];
+    const uint32_t n0 = (uint32_t)(p1 >> 32) ^ w[1] ^ k0, n2 = (uint32_t)(p0 >> 32) ^ w[3] ^ k1;
+    w[1] = (uint32_t)p1; w[3] = (uint32_t)p0;
+    w[0] = n0; w[2] = n2;
+    k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
+  }
+}
+// Elements first .. first + 7 of the dense matrix: what is kept times d.factor, the rest 0.  A dropped element is not
+// multiplied, so that what it held, an infinity say, is gone.
+__device__ __forceinline__ void drop8(const Drop& d, const DropKey& key, uint64_t first, float (&v)[8]) {
+  uint32_t w[4];
+  const uint32_t skew = (uint32_t)first & 7u;
+  philox7(key, first >> 3, w);
+  if (skew == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t half = (i & 1) ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu;
+      v[i] = half < d.limit ? 0.0f : v[i] * d.factor;
+    }
+  } else {  // an odd number of columns: the eight lie in two blocks of the generator
+    uint32_t u[4];
+    philox7(key, (first >> 3) + 1, u);
+    // one bit per half-word of both blocks, then eight of the sixteen
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bits |= ((w[i] & 0xffffu) < d.limit ? 0u : 1u) << (2 * i);
+      bits |= ((w[i] >> 16) < d.limit ? 0u : 1u) << (2 * i + 1);
+      bits |= ((u[i] & 0xffffu) < d.limit ? 0u : 1u) << (2 * i + 8);
+      bits |= ((u[i] >> 16) < d.limit ? 0u : 1u) << (2 * i + 9);
+    }
+    bits >>= skew;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (bits >> i) & 1u ? v[i] * d.factor : 0.0f;
+  }
+}
+// drop(v) times the scale: also where nothing is dropped
+__device__ __forceinline__ void scale_drop8(const Drop& d, const DropKey& key, uint64_t first, float (&v)[8]) {
+  if (d.limit) {
+    drop8(d, key, first, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= d.factor;
+  }
+}
+
+}  // namespace layers
+}  // namespace triaccel

@@ -1,0 +1,87 @@
+// Launchers of the layer operators' kernels, called by layers_api.hip.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gemm_plan.h"
+
+namespace triaccel {
+namespace layers {
+
+struct GemmArgs;
+struct Drop;
+
+enum Product : int { kForward = 0, kGatedForward = 1, kInputGrad = 2, kWeightGrad = 3 };
+
+hipError_t launch_gemm_fp16(Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t stream);
+hipError_t launch_gemm_bf16(Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t stream);
+hipError_t launch_gemm_fp32(Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t stream);
+
+// The gradient before the activation, and its sums over the rows.
+struct SlopeArgs {
+  const void *dy, *gate, *up;   // linear: gate = pre, up unused
+  int64_t lddy, ldg;
+  int64_t rows, cols, width;    // width: cols rounded up to the columns that dz has in the workspace
+  void *dz;                     // NULL: sums only.  gated: rows x (2 width), dg and du side by side
+  float *sums;                  // [blocks][cols] (gated: [blocks][2 cols]), or NULL
+  int64_t rows_per_block;
+  int32_t act, blocks;
+  const Drop* drop;             // linear only (host pointer)
+};
+hipError_t launch_slope(int dtype, bool gated, const SlopeArgs& a, hipStream_t stream);
+
+// out[v][c] = sum over blocks of sums[block][v * cols + c], for up to five vectors v; NULL vectors are left out.
+struct ColumnSums {
+  const float* sums;
+  int64_t cols, stride;  // stride: values of a block
+  int32_t blocks, vectors, dtype;
+  void* out[5];
+};
+hipError_t launch_column_sums(const ColumnSums& a, hipStream_t stream);
+
+struct NormSide {
+  const void *weight, *bias;
+  int32_t kind, dtype;
+  float eps;
+};
+struct NormArgs {
+  int64_t rows, cols;
+  const void *r, *b, *gate;
+  int64_t ldr, ldb, ldgate, rows_per_gate;
+  void *ro, *y;
+  int64_t ldro, ldy;
+  int32_t gate_dtype;
+  float scale;
+  NormSide post, norm;
+};
+hipError_t launch_residual_norm(int dtype, const NormArgs& a, hipStream_t stream);
+
+struct NormGradArgs {
+  int64_t rows, cols;
+  const void *dro, *dy, *r, *b, *gate;
+  int64_t lddro, lddy, ldr, ldb, ldgate, rows_per_gate;
+  void *dr, *db;
+  int64_t lddr, lddb;
+  int32_t gate_dtype, vec_dtype;
+  float scale;
+  NormSide post, norm;
+  float* sums;            // [teams][vectors][cols]
+  float* gate_edges;      // [teams][2][cols]: gates of groups of rows that a team has a part of
+  void *dgate, *dpw, *dpb, *dnw, *dnb;
+  int32_t teams;
+  int64_t rows_per_team;
+};
+constexpr int kNormVectors = 5;  // dnw, dnb, dpw, dpb, dgate
+void norm_grad_teams(int64_t rows, int64_t cols, int32_t& teams, int64_t& rows_per_team);
+hipError_t launch_residual_norm_grad(int dtype, const NormGradArgs& a, hipStream_t stream);
+
+struct DropoutArgs {
+  int64_t rows, cols;
+  const void *x, *r;
+  int64_t ldx, ldr, ldy;
+  void* y;
+};
+hipError_t launch_dropout(int dtype, const DropoutArgs& a, const Drop& d, hipStream_t stream);
+
+}  // namespace layers
+}  // namespace triaccel

@@ -1,0 +1,491 @@
+// Host side of include/triaccel_layers.h: checks of arguments, layout of the workspace, order of the launches.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdio>
+
+#include "../../../include/triaccel_layers.h"
+#include "../kernels.h"
+#include "gemm.h"
+#include "gemm_plan.h"
+#include "layers.h"
+
+using namespace triaccel;
+using namespace triaccel::layers;
+
+namespace {
+
+constexpr int64_t kMaxDim = 0x7fffffff;
+
+int refuse(int code, const char* text) {
+  note_error(text);
+  return code;
+}
+int hip_status(hipError_t e, const char* what) {
+  if (e == hipSuccess) return TRIACCEL_OK;
+  char text[256];
+  snprintf(text, sizeof text, "%s: %s", what, hipGetErrorString(e));
+  return refuse(TRIACCEL_E_HIP, text);
+}
+#define TA_TRY(expr)              \
+  do {                            \
+    const int rc_ = (expr);       \
+    if (rc_ != TRIACCEL_OK) return rc_; \
+  } while (0)
+
+bool valid_dtype(int32_t d) { return d == TRIACCEL_FP16 || d == TRIACCEL_BF16 || d == TRIACCEL_FP32; }
+int64_t bytes_of(int32_t dtype) { return dtype == TRIACCEL_FP32 ? 4 : 2; }
+
+// A matrix of `rows` rows of `cols` elements: where it has rows it has an address, at its element's alignment, and rows that
+// do not overlap.
+int check_matrix(const void* p, int64_t ld, int64_t rows, int64_t cols, int32_t dtype, const char* name) {
+  char text[96];
+  if (rows > 0 && !p) {
+    snprintf(text, sizeof text, "%s is NULL", name);
+    return refuse(TRIACCEL_E_NULL_PTR, text);
+  }
+  if (ld < cols || ld > kMaxDim) {
+    snprintf(text, sizeof text, "the row stride of %s is below its columns, or too large", name);
+    return refuse(TRIACCEL_E_INVALID_ARG, text);
+  }
+  if (reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes_of(dtype)) {
+    snprintf(text, sizeof text, "%s is not aligned to its elements", name);
+    return refuse(TRIACCEL_E_ALIGNMENT, text);
+  }
+  return TRIACCEL_OK;
+}
+int check_vector(const void* p, int32_t dtype, const char* name) {
+  if (!p) return TRIACCEL_OK;
+  if (!valid_dtype(dtype)) return refuse(TRIACCEL_E_BAD_DTYPE, name);
+  return check_matrix(p, 1, 1, 1, dtype, name);
+}
+int check_sizes(int32_t dtype, int64_t rows, int64_t a, int64_t b) {
+  if (!valid_dtype(dtype)) return refuse(TRIACCEL_E_BAD_DTYPE, "dtype");
+  if (rows < 0 || a < 1 || b < 1 || rows > kMaxDim || a > kMaxDim || b > kMaxDim)
+    return refuse(TRIACCEL_E_INVALID_ARG, "sizes: rows >= 0, columns >= 1, all below 2^31");
+  return TRIACCEL_OK;
+}
+int check_drop(const triaccel_dropout_spec& d, float scale) {
+  if (!(d.p >= 0.0 && d.p < 1.0)) return refuse(TRIACCEL_E_INVALID_ARG, "dropout: p is outside [0, 1)");
+  if (!std::isfinite(scale)) return refuse(TRIACCEL_E_INVALID_ARG, "scale is not finite");
+  if (reinterpret_cast<uintptr_t>(d.device_seed) & 7u) return refuse(TRIACCEL_E_ALIGNMENT, "device_seed is not aligned to 8 bytes");
+  return TRIACCEL_OK;
+}
+Drop drop_of(const triaccel_dropout_spec& d, float scale) {
+  const double t = std::nearbyint(d.p * 65536.0);
+  const uint32_t limit = t > 65535.0 ? 65535u : (uint32_t)t;
+  return Drop{d.seed, d.offset, d.device_seed, limit, (float)((double)scale * 65536.0 / (65536.0 - limit))};
+}
+int check_act(int32_t act, bool none) {
+  if (act < (none ? TRIACCEL_ACT_NONE : TRIACCEL_ACT_RELU) || act > TRIACCEL_ACT_GELU_TANH)
+    return refuse(TRIACCEL_E_INVALID_ARG, "act: no such activation");
+  return TRIACCEL_OK;
+}
+int check_workspace(const void* p, uint64_t has, uint64_t needs) {
+  if (has < needs || (needs && !p)) return refuse(TRIACCEL_E_INVALID_ARG, "the workspace is smaller than the call's _workspace size");
+  if (reinterpret_cast<uintptr_t>(p) & 15u) return refuse(TRIACCEL_E_ALIGNMENT, "the workspace is not 16-byte aligned");
+  return TRIACCEL_OK;
+}
+
+uint64_t padded(uint64_t bytes) { return (bytes + 255u) & ~(uint64_t)255u; }
+
+// ---- products ------------------------------------------------------------------------------------------------------
+
+hipError_t run_product(int32_t dtype, Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t s) {
+  return dtype == TRIACCEL_FP16 ? launch_gemm_fp16(kind, p, direct, g, s)
+         : dtype == TRIACCEL_BF16 ? launch_gemm_bf16(kind, p, direct, g, s) : launch_gemm_fp32(kind, p, direct, g, s);
+}
+
+// Whether an operand's 16-byte units can go straight to LDS: units whole and aligned (`whole`: the contiguous length ends with a
+// unit, or its rows have room for the last), and a tile's rows within 31 bits of its first.
+bool direct_ok(const void* p, int64_t ld, bool whole) {
+  return whole && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0 && ld < (1 << 21);
+}
+GemmPlan plan_of(int32_t dtype, Product kind, bool direct, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
+  return plan_gemm(dtype == TRIACCEL_FP32, kind == kGatedForward, direct, m, n, seg, nseg);
+}
+// The workspace does not depend on alignment: the larger of both plans.
+uint64_t partial_bytes(int32_t dtype, Product kind, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
+  const uint64_t a = plan_of(dtype, kind, true, m, n, seg, nseg).partial_bytes, b = plan_of(dtype, kind, false, m, n, seg, nseg).partial_bytes;
+  return padded(a > b ? a : b);
+}
+
+// ---- gradients before the activation ---------------------------------------------------------------------------------
+
+struct BackwardLayout {
+  int64_t width;
+  uint64_t dz, sums, partial, total;
+  int32_t blocks;
+  int64_t rows_per_block;
+};
+// `dz_needed`: dz is not dy itself.  `wide`: 2 for the gated block.
+BackwardLayout backward_layout(int32_t dtype, int64_t rows, int64_t in, int64_t out, bool dz_needed, bool sums, bool dx, bool dw, int64_t wide) {
+  BackwardLayout l{};
+  l.width = (out + 7) / 8 * 8;
+  // 64 rows a workgroup, more where that makes over 128 blocks (their sums are added up by one workgroup per 64 columns)
+  l.rows_per_block = 64;
+  if (ceil_div(rows, l.rows_per_block) > 128) l.rows_per_block = ceil_div(rows, 128);
+  l.blocks = (int32_t)ceil_div(rows, l.rows_per_block);
+  l.dz = 0;
+  l.sums = dz_needed ? padded((uint64_t)rows * (uint64_t)(wide * l.width) * (uint64_t)bytes_of(dtype)) : 0;
+  l.partial = l.sums + (sums ? padded((uint64_t)l.blocks * (uint64_t)(wide * out) * 4u) : 0);
+  const uint64_t a = dx ? partial_bytes(dtype, kInputGrad, rows, in, out, wide) : 0;
+  const uint64_t b = dw ? partial_bytes(dtype, kWeightGrad, wide == 2 ? l.width + out : out, in, rows, 1) : 0;
+  l.total = l.partial + (a > b ? a : b);
+  return l;
+}
+
+// dx = dz W (gated: dg Wg + du Wu) and dW = dz^T x from dz as it lies (ld: its rows' distance; gated: du `step` behind dg).
+struct BackwardProducts {
+  int32_t dtype;
+  int64_t rows, in, out;
+  const void *dz;
+  int64_t ld, step;
+  bool dz_padded;
+  const void *x, *w, *w2;
+  int64_t ldx, ldw;
+  void *dx, *dw, *dw2;
+  int64_t lddx, lddw;
+  int32_t dw_dtype;
+  float* partial;
+};
+int backward_products(const BackwardProducts& q, hipStream_t s) {
+  const int64_t wide = q.w2 || q.dw2 ? 2 : 1;
+  if (q.dx && q.rows > 0) {
+    const bool direct = q.dtype != TRIACCEL_FP32 && direct_ok(q.dz, q.ld, q.dz_padded || q.out % 8 == 0) && q.step % 8 == 0 &&
+                        direct_ok(q.w, q.ldw, q.in % 8 == 0) && (!q.w2 || direct_ok(q.w2, q.ldw, true));
+    const GemmPlan p = plan_of(q.dtype, kInputGrad, direct, q.rows, q.in, q.out, wide);
+    GemmArgs g{};
+    g.a = q.dz; g.lda = q.ld; g.b = q.w; g.b2 = q.w2; g.ldb = q.ldw;
+    g.m = (int32_t)q.rows; g.n = (int32_t)q.in; g.seg = (int32_t)q.out; g.nseg = (int32_t)wide; g.seg_step = (int32_t)q.step;
+    g.partial = q.partial;
+    g.c = q.dx; g.ldc = q.lddx; g.crows = g.csplit = 0x7fffffff; g.c_fp32 = q.dtype == TRIACCEL_FP32;
+    TA_TRY(hip_status(run_product(q.dtype, kInputGrad, p, direct, g, s), "gradient of the input"));
+  }
+  if (q.dw) {
+    // no rows: the product has no terms and its result is zero
+    const bool direct = q.dtype != TRIACCEL_FP32 && direct_ok(q.dz, q.ld, q.dz_padded || q.out % 8 == 0) && q.step % 8 == 0 &&
+                        direct_ok(q.x, q.ldx, q.in % 8 == 0);
+    const int64_t m = wide == 2 ? q.step + q.out : q.out;
+    const GemmPlan p = plan_of(q.dtype, kWeightGrad, direct, m, q.in, q.rows, 1);
+    GemmArgs g{};
+    g.a = q.dz; g.lda = q.ld; g.b = q.x; g.ldb = q.ldx;
+    g.m = (int32_t)m; g.n = (int32_t)q.in; g.seg = (int32_t)q.rows; g.nseg = 1;
+    g.partial = q.partial;
+    g.c = q.dw; g.c2 = q.dw2; g.ldc = q.lddw; g.crows = (int32_t)q.out; g.csplit = wide == 2 ? (int32_t)q.step : 0x7fffffff;
+    g.c_fp32 = q.dw_dtype == TRIACCEL_FP32;
+    TA_TRY(hip_status(run_product(q.dtype, kWeightGrad, p, direct, g, s), "gradient of the weights"));
+  }
+  return TRIACCEL_OK;
+}
+
+bool slope_needed(const triaccel_linear_backward_args& a) { return a.act != TRIACCEL_ACT_NONE || a.drop.p > 0.0 || a.scale != 1.0f; }
+
+int check_linear(const triaccel_linear_args* a) {
+  if (!a) return refuse(TRIACCEL_E_NULL_PTR, "args is NULL");
+  if (a->struct_size != sizeof(*a)) return refuse(TRIACCEL_E_INVALID_ARG, "struct_size");
+  TA_TRY(check_sizes(a->dtype, a->rows, a->in, a->out));
+  TA_TRY(check_act(a->act, true));
+  return check_drop(a->drop, a->scale);
+}
+int check_linear_backward(const triaccel_linear_backward_args* a) {
+  if (!a) return refuse(TRIACCEL_E_NULL_PTR, "args is NULL");
+  if (a->struct_size != sizeof(*a)) return refuse(TRIACCEL_E_INVALID_ARG, "struct_size");
+  TA_TRY(check_sizes(a->dtype, a->rows, a->in, a->out));
+  TA_TRY(check_act(a->act, true));
+  if (a->dweight_dtype != a->dtype && a->dweight_dtype != TRIACCEL_FP32)
+    return refuse(TRIACCEL_E_BAD_DTYPE, "dweight_dtype is neither the call's dtype nor FP32");
+  return check_drop(a->drop, a->scale);
+}
+int check_gated(const triaccel_gated_args* a) {
+  if (!a) return refuse(TRIACCEL_E_NULL_PTR, "args is NULL");
+  if (a->struct_size != sizeof(*a)) return refuse(TRIACCEL_E_INVALID_ARG, "struct_size");
+  TA_TRY(check_sizes(a->dtype, a->rows, a->in, a->out));
+  if (a->out > kMaxDim / 2 - 16) return refuse(TRIACCEL_E_INVALID_ARG, "out: below 2^30 in a gated block");
+  return check_act(a->act, false);
+}
+int check_gated_backward(const triaccel_gated_backward_args* a) {
+  if (!a) return refuse(TRIACCEL_E_NULL_PTR, "args is NULL");
+  if (a->struct_size != sizeof(*a)) return refuse(TRIACCEL_E_INVALID_ARG, "struct_size");
+  TA_TRY(check_sizes(a->dtype, a->rows, a->in, a->out));
+  if (a->out > kMaxDim / 2 - 16) return refuse(TRIACCEL_E_INVALID_ARG, "out: below 2^30 in a gated block");
+  if (a->dweight_dtype != a->dtype && a->dweight_dtype != TRIACCEL_FP32)
+    return refuse(TRIACCEL_E_BAD_DTYPE, "dweight_dtype is neither the call's dtype nor FP32");
+  return check_act(a->act, false);
+}
+
+// ---- norms -----------------------------------------------------------------------------------------------------------
+
+int check_norm(const triaccel_norm_spec& n, const char* name) {
+  if (n.kind < TRIACCEL_NORM_NONE || n.kind > TRIACCEL_NORM_LAYER) return refuse(TRIACCEL_E_INVALID_ARG, "norm: no such kind");
+  if (n.kind == TRIACCEL_NORM_NONE) return TRIACCEL_OK;
+  if (!(n.eps > 0.0f) || !std::isfinite(n.eps)) return refuse(TRIACCEL_E_INVALID_ARG, "norm: eps is not above 0");
+  TA_TRY(check_vector(n.weight, n.dtype, name));
+  return check_vector(n.bias, n.dtype, name);
+}
+NormSide side_of(const triaccel_norm_spec& n) { return NormSide{n.weight, n.bias, n.kind, n.dtype, n.eps}; }
+int check_gate(const void* gate, int64_t ld, int64_t rows_per_gate, int64_t cols, int32_t dtype) {
+  if (rows_per_gate < 0) return refuse(TRIACCEL_E_INVALID_ARG, "rows_per_gate is below 0");
+  TA_TRY(check_vector(gate, dtype, "gate"));
+  if (gate && rows_per_gate > 0) return check_matrix(gate, ld, 1, cols, dtype, "gate");
+  return TRIACCEL_OK;
+}
+int check_norm_backward(const triaccel_residual_norm_backward_args* a) {
+  if (!a) return refuse(TRIACCEL_E_NULL_PTR, "args is NULL");
+  if (a->struct_size != sizeof(*a)) return refuse(TRIACCEL_E_INVALID_ARG, "struct_size");
+  TA_TRY(check_sizes(a->dtype, a->rows, a->cols, 1));
+  if (a->cols > TRIACCEL_NORM_MAX_COLS) return refuse(TRIACCEL_E_INVALID_ARG, "cols: above TRIACCEL_NORM_MAX_COLS");
+  if (a->rows_per_gate < 0) return refuse(TRIACCEL_E_INVALID_ARG, "rows_per_gate is below 0");
+  return TRIACCEL_OK;
+}
+struct NormLayout {
+  int32_t teams;
+  int64_t rows_per_team;
+  uint64_t edges, total;
+};
+NormLayout norm_layout(const triaccel_residual_norm_backward_args& a) {
+  NormLayout l{};
+  norm_grad_teams(a.rows, a.cols, l.teams, l.rows_per_team);
+  const bool grouped = a.dgate && a.rows_per_gate > 0;
+  const bool sums = a.dnorm_weight || a.dnorm_bias || a.dpost_weight || a.dpost_bias || (a.dgate && !grouped);
+  l.edges = sums ? padded((uint64_t)l.teams * kNormVectors * (uint64_t)a.cols * 4u) : 0;
+  l.total = l.edges + (grouped ? padded((uint64_t)l.teams * 2u * (uint64_t)a.cols * 4u) : 0);
+  return l;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t triaccel_linear_workspace(const triaccel_linear_args* a) {
+  TA_TRY(check_linear(a));
+  return a->rows ? (int64_t)partial_bytes(a->dtype, kForward, a->rows, a->out, a->in, 1) : 0;
+}
+
+int triaccel_linear(const triaccel_linear_args* a, void* hip_stream) {
+  TA_TRY(check_linear(a));
+  TA_TRY(check_matrix(a->x, a->ldx, a->rows, a->in, a->dtype, "x"));
+  TA_TRY(check_matrix(a->weight, a->ldw, a->out, a->in, a->dtype, "weight"));
+  TA_TRY(check_vector(a->bias, a->bias_dtype, "bias"));
+  if (a->residual) TA_TRY(check_matrix(a->residual, a->ldr, a->rows, a->out, a->dtype, "residual"));
+  TA_TRY(check_matrix(a->y, a->ldy, a->rows, a->out, a->dtype, "y"));
+  if (a->pre) TA_TRY(check_matrix(a->pre, a->ldpre, a->rows, a->out, a->dtype, "pre"));
+  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, (uint64_t)triaccel_linear_workspace(a)));
+  if (a->rows == 0) return TRIACCEL_OK;
+  const bool direct = a->dtype != TRIACCEL_FP32 && direct_ok(a->x, a->ldx, a->in % 8 == 0) && direct_ok(a->weight, a->ldw, true);
+  const GemmPlan p = plan_of(a->dtype, kForward, direct, a->rows, a->out, a->in, 1);
+  GemmArgs g{};
+  g.a = a->x; g.lda = a->ldx; g.b = a->weight; g.ldb = a->ldw;
+  g.m = (int32_t)a->rows; g.n = (int32_t)a->out; g.seg = (int32_t)a->in; g.nseg = 1;
+  g.partial = (float*)a->workspace;
+  g.c = a->y; g.ldc = a->ldy; g.pre = a->pre; g.ldpre = a->ldpre;
+  g.bias = a->bias; g.bias_dtype = a->bias_dtype; g.act = a->act;
+  g.residual = a->residual; g.ldr = a->ldr;
+  g.drop = drop_of(a->drop, a->scale);
+  return hip_status(run_product(a->dtype, kForward, p, direct, g, (hipStream_t)hip_stream), "linear");
+}
+
+int64_t triaccel_linear_backward_workspace(const triaccel_linear_backward_args* a) {
+  TA_TRY(check_linear_backward(a));
+  return (int64_t)backward_layout(a->dtype, a->rows, a->in, a->out, slope_needed(*a) && (a->dx || a->dweight), a->dbias, a->dx, a->dweight, 1).total;
+}
+
+int triaccel_linear_backward(const triaccel_linear_backward_args* a, void* hip_stream) {
+  TA_TRY(check_linear_backward(a));
+  TA_TRY(check_matrix(a->dy, a->lddy, a->rows, a->out, a->dtype, "dy"));
+  if (a->dweight) TA_TRY(check_matrix(a->x, a->ldx, a->rows, a->in, a->dtype, "x"));
+  if (a->dx) TA_TRY(check_matrix(a->weight, a->ldw, a->out, a->in, a->dtype, "weight"));
+  if (a->act != TRIACCEL_ACT_NONE) TA_TRY(check_matrix(a->pre, a->ldpre, a->rows, a->out, a->dtype, "pre"));
+  if (a->dx) TA_TRY(check_matrix(a->dx, a->lddx, a->rows, a->in, a->dtype, "dx"));
+  if (a->dweight) TA_TRY(check_matrix(a->dweight, a->lddw, a->out, a->in, a->dweight_dtype, "dweight"));
+  TA_TRY(check_vector(a->dbias, a->dbias_dtype, "dbias"));
+  const bool slope = slope_needed(*a) && (a->dx || a->dweight);
+  const BackwardLayout l = backward_layout(a->dtype, a->rows, a->in, a->out, slope, a->dbias, a->dx, a->dweight, 1);
+  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, l.total));
+  char* ws = (char*)a->workspace;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const Drop drop = drop_of(a->drop, a->scale);
+  if ((slope || a->dbias) && a->rows > 0) {
+    SlopeArgs q{};
+    q.dy = a->dy; q.lddy = a->lddy; q.gate = a->pre; q.ldg = a->ldpre;
+    q.rows = a->rows; q.cols = a->out; q.width = l.width;
+    q.dz = slope ? ws + l.dz : nullptr;
+    q.sums = a->dbias ? (float*)(ws + l.sums) : nullptr;
+    q.rows_per_block = l.rows_per_block; q.blocks = l.blocks; q.act = a->act; q.drop = &drop;
+    TA_TRY(hip_status(launch_slope(a->dtype, false, q, s), "gradient before the activation"));
+  }
+  if (a->dbias) {
+    ColumnSums c{(const float*)(ws + l.sums), a->out, a->out, l.blocks, 1, a->dbias_dtype, {a->dbias}};
+    TA_TRY(hip_status(launch_column_sums(c, s), "gradient of the bias"));
+  }
+  BackwardProducts q{};
+  q.dtype = a->dtype; q.rows = a->rows; q.in = a->in; q.out = a->out;
+  q.dz = slope ? (const void*)(ws + l.dz) : a->dy; q.ld = slope ? l.width : a->lddy; q.dz_padded = slope;
+  q.x = a->x; q.ldx = a->ldx; q.w = a->weight; q.ldw = a->ldw;
+  q.dx = a->dx; q.lddx = a->lddx; q.dw = a->dweight; q.lddw = a->lddw; q.dw_dtype = a->dweight_dtype;
+  q.partial = (float*)(ws + l.partial);
+  return backward_products(q, s);
+}
+
+int64_t triaccel_gated_workspace(const triaccel_gated_args* a) {
+  TA_TRY(check_gated(a));
+  return a->rows ? (int64_t)partial_bytes(a->dtype, kGatedForward, a->rows, a->out, a->in, 1) : 0;
+}
+
+int triaccel_gated(const triaccel_gated_args* a, void* hip_stream) {
+  TA_TRY(check_gated(a));
+  TA_TRY(check_matrix(a->x, a->ldx, a->rows, a->in, a->dtype, "x"));
+  TA_TRY(check_matrix(a->w_gate, a->ldw, a->out, a->in, a->dtype, "w_gate"));
+  TA_TRY(check_matrix(a->w_up, a->ldw, a->out, a->in, a->dtype, "w_up"));
+  if (!a->b_gate != !a->b_up) return refuse(TRIACCEL_E_NULL_PTR, "b_gate and b_up come together");
+  TA_TRY(check_vector(a->b_gate, a->bias_dtype, "b_gate"));
+  TA_TRY(check_vector(a->b_up, a->bias_dtype, "b_up"));
+  TA_TRY(check_matrix(a->h, a->ldh, a->rows, a->out, a->dtype, "h"));
+  if (!a->gate != !a->up) return refuse(TRIACCEL_E_NULL_PTR, "gate and up come together");
+  if (a->gate) {
+    TA_TRY(check_matrix(a->gate, a->ldg, a->rows, a->out, a->dtype, "gate"));
+    TA_TRY(check_matrix(a->up, a->ldg, a->rows, a->out, a->dtype, "up"));
+  }
+  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, (uint64_t)triaccel_gated_workspace(a)));
+  if (a->rows == 0) return TRIACCEL_OK;
+  const bool direct = a->dtype != TRIACCEL_FP32 && direct_ok(a->x, a->ldx, a->in % 8 == 0) && direct_ok(a->w_gate, a->ldw, true) &&
+                      direct_ok(a->w_up, a->ldw, true);
+  const GemmPlan p = plan_of(a->dtype, kGatedForward, direct, a->rows, a->out, a->in, 1);
+  GemmArgs g{};
+  g.a = a->x; g.lda = a->ldx; g.b = a->w_gate; g.b2 = a->w_up; g.ldb = a->ldw;
+  g.m = (int32_t)a->rows; g.n = (int32_t)a->out; g.seg = (int32_t)a->in; g.nseg = 1;
+  g.partial = (float*)a->workspace;
+  g.c = a->h; g.ldc = a->ldh; g.pre = a->gate; g.pre2 = a->up; g.ldpre = a->ldg;
+  g.bias = a->b_gate; g.bias2 = a->b_up; g.bias_dtype = a->bias_dtype; g.act = a->act;
+  return hip_status(run_product(a->dtype, kGatedForward, p, direct, g, (hipStream_t)hip_stream), "gated");
+}
+
+int64_t triaccel_gated_backward_workspace(const triaccel_gated_backward_args* a) {
+  TA_TRY(check_gated_backward(a));
+  return (int64_t)backward_layout(a->dtype, a->rows, a->in, a->out, a->dx || a->dw_gate, a->db_gate, a->dx, a->dw_gate, 2).total;
+}
+
+int triaccel_gated_backward(const triaccel_gated_backward_args* a, void* hip_stream) {
+  TA_TRY(check_gated_backward(a));
+  TA_TRY(check_matrix(a->dh, a->lddh, a->rows, a->out, a->dtype, "dh"));
+  TA_TRY(check_matrix(a->gate, a->ldg, a->rows, a->out, a->dtype, "gate"));
+  TA_TRY(check_matrix(a->up, a->ldg, a->rows, a->out, a->dtype, "up"));
+  if (!a->dw_gate != !a->dw_up) return refuse(TRIACCEL_E_NULL_PTR, "dw_gate and dw_up come together");
+  if (!a->db_gate != !a->db_up) return refuse(TRIACCEL_E_NULL_PTR, "db_gate and db_up come together");
+  if (a->dw_gate) {
+    TA_TRY(check_matrix(a->x, a->ldx, a->rows, a->in, a->dtype, "x"));
+    TA_TRY(check_matrix(a->dw_gate, a->lddw, a->out, a->in, a->dweight_dtype, "dw_gate"));
+    TA_TRY(check_matrix(a->dw_up, a->lddw, a->out, a->in, a->dweight_dtype, "dw_up"));
+  }
+  if (a->dx) {
+    TA_TRY(check_matrix(a->w_gate, a->ldw, a->out, a->in, a->dtype, "w_gate"));
+    TA_TRY(check_matrix(a->w_up, a->ldw, a->out, a->in, a->dtype, "w_up"));
+    TA_TRY(check_matrix(a->dx, a->lddx, a->rows, a->in, a->dtype, "dx"));
+  }
+  TA_TRY(check_vector(a->db_gate, a->dbias_dtype, "db_gate"));
+  TA_TRY(check_vector(a->db_up, a->dbias_dtype, "db_up"));
+  const bool products = a->dx || a->dw_gate;
+  const BackwardLayout l = backward_layout(a->dtype, a->rows, a->in, a->out, products, a->db_gate, a->dx, a->dw_gate, 2);
+  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, l.total));
+  char* ws = (char*)a->workspace;
+  hipStream_t s = (hipStream_t)hip_stream;
+  if ((products || a->db_gate) && a->rows > 0) {
+    SlopeArgs q{};
+    q.dy = a->dh; q.lddy = a->lddh; q.gate = a->gate; q.up = a->up; q.ldg = a->ldg;
+    q.rows = a->rows; q.cols = a->out; q.width = l.width;
+    q.dz = products ? ws + l.dz : nullptr;
+    q.sums = a->db_gate ? (float*)(ws + l.sums) : nullptr;
+    q.rows_per_block = l.rows_per_block; q.blocks = l.blocks; q.act = a->act;
+    TA_TRY(hip_status(launch_slope(a->dtype, true, q, s), "gradients before the activation"));
+  }
+  if (a->db_gate) {
+    ColumnSums c{(const float*)(ws + l.sums), a->out, 2 * a->out, l.blocks, 2, a->dbias_dtype, {a->db_gate, a->db_up}};
+    TA_TRY(hip_status(launch_column_sums(c, s), "gradients of the biases"));
+  }
+  BackwardProducts q{};
+  q.dtype = a->dtype; q.rows = a->rows; q.in = a->in; q.out = a->out;
+  q.dz = ws + l.dz; q.ld = 2 * l.width; q.step = l.width; q.dz_padded = true;
+  q.x = a->x; q.ldx = a->ldx; q.w = a->w_gate; q.w2 = a->w_up; q.ldw = a->ldw;
+  q.dx = a->dx; q.lddx = a->lddx; q.dw = a->dw_gate; q.dw2 = a->dw_up; q.lddw = a->lddw; q.dw_dtype = a->dweight_dtype;
+  q.partial = (float*)(ws + l.partial);
+  return backward_products(q, s);
+}
+
+int triaccel_residual_norm(const triaccel_residual_norm_args* a, void* hip_stream) {
+  if (!a) return refuse(TRIACCEL_E_NULL_PTR, "args is NULL");
+  if (a->struct_size != sizeof(*a)) return refuse(TRIACCEL_E_INVALID_ARG, "struct_size");
+  TA_TRY(check_sizes(a->dtype, a->rows, a->cols, 1));
+  if (a->cols > TRIACCEL_NORM_MAX_COLS) return refuse(TRIACCEL_E_INVALID_ARG, "cols: above TRIACCEL_NORM_MAX_COLS");
+  if (!std::isfinite(a->scale)) return refuse(TRIACCEL_E_INVALID_ARG, "scale is not finite");
+  TA_TRY(check_norm(a->post, "post norm"));
+  TA_TRY(check_norm(a->norm, "norm"));
+  TA_TRY(check_gate(a->gate, a->ldgate, a->rows_per_gate, a->cols, a->gate_dtype));
+  TA_TRY(check_matrix(a->residual, a->ldr, a->rows, a->cols, a->dtype, "residual"));
+  if (a->block) {
+    TA_TRY(check_matrix(a->block, a->ldb, a->rows, a->cols, a->dtype, "block"));
+    TA_TRY(check_matrix(a->residual_out, a->ldro, a->rows, a->cols, a->dtype, "residual_out"));
+  }
+  if (a->norm.kind != TRIACCEL_NORM_NONE) TA_TRY(check_matrix(a->y, a->ldy, a->rows, a->cols, a->dtype, "y"));
+  if (a->rows == 0) return TRIACCEL_OK;
+  const NormArgs n{a->rows, a->cols, a->residual, a->block, a->gate, a->ldr, a->ldb, a->ldgate, a->rows_per_gate, a->residual_out, a->y,
+                   a->ldro, a->ldy, a->gate_dtype, a->scale, side_of(a->post), side_of(a->norm)};
+  return hip_status(launch_residual_norm(a->dtype, n, (hipStream_t)hip_stream), "residual_norm");
+}
+
+int64_t triaccel_residual_norm_backward_workspace(const triaccel_residual_norm_backward_args* a) {
+  TA_TRY(check_norm_backward(a));
+  return (int64_t)norm_layout(*a).total;
+}
+
+int triaccel_residual_norm_backward(const triaccel_residual_norm_backward_args* a, void* hip_stream) {
+  TA_TRY(check_norm_backward(a));
+  if (!std::isfinite(a->scale)) return refuse(TRIACCEL_E_INVALID_ARG, "scale is not finite");
+  TA_TRY(check_norm(a->post, "post norm"));
+  TA_TRY(check_norm(a->norm, "norm"));
+  TA_TRY(check_gate(a->gate, a->ldgate, a->rows_per_gate, a->cols, a->gate_dtype));
+  if (a->dresidual_out) TA_TRY(check_matrix(a->dresidual_out, a->lddro, a->rows, a->cols, a->dtype, "dresidual_out"));
+  if (a->norm.kind != TRIACCEL_NORM_NONE && a->dy) {
+    TA_TRY(check_matrix(a->dy, a->lddy, a->rows, a->cols, a->dtype, "dy"));
+    TA_TRY(check_matrix(a->residual, a->ldr, a->rows, a->cols, a->dtype, "residual"));
+  }
+  const bool block_side = a->dblock || a->dgate || a->dpost_weight || a->dpost_bias;
+  if (a->block || block_side) TA_TRY(check_matrix(a->block, a->ldb, a->rows, a->cols, a->dtype, "block"));
+  if (a->dresidual) TA_TRY(check_matrix(a->dresidual, a->lddr, a->rows, a->cols, a->dtype, "dresidual"));
+  if (a->dblock) TA_TRY(check_matrix(a->dblock, a->lddb, a->rows, a->cols, a->dtype, "dblock"));
+  if ((a->dpost_weight || a->dpost_bias) && a->post.kind == TRIACCEL_NORM_NONE)
+    return refuse(TRIACCEL_E_INVALID_ARG, "gradients of a norm after the block that the call does not have");
+  if ((a->dnorm_weight || a->dnorm_bias) && a->norm.kind == TRIACCEL_NORM_NONE)
+    return refuse(TRIACCEL_E_INVALID_ARG, "gradients of a norm that the call does not have");
+  if (a->dgate && !a->gate) return refuse(TRIACCEL_E_NULL_PTR, "dgate without a gate");
+  for (const void* v : {a->dgate, a->dpost_weight, a->dpost_bias, a->dnorm_weight, a->dnorm_bias}) TA_TRY(check_vector(v, a->dvec_dtype, "a vector's gradient"));
+  const NormLayout l = norm_layout(*a);
+  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, l.total));
+  hipStream_t s = (hipStream_t)hip_stream;
+  if (a->rows == 0) {
+    ColumnSums none{nullptr, a->cols, 0, 0, kNormVectors, a->dvec_dtype,
+                    {a->dnorm_weight, a->dnorm_bias, a->dpost_weight, a->dpost_bias, a->rows_per_gate ? nullptr : a->dgate}};
+    return hip_status(launch_column_sums(none, s), "residual_norm_backward");
+  }
+  char* ws = (char*)a->workspace;
+  const NormGradArgs n{a->rows, a->cols, a->dresidual_out, a->dy, a->residual, a->block, a->gate, a->lddro, a->lddy, a->ldr, a->ldb, a->ldgate,
+                       a->rows_per_gate, a->dresidual, a->dblock, a->lddr, a->lddb, a->gate_dtype, a->dvec_dtype, a->scale, side_of(a->post),
+                       side_of(a->norm), l.edges ? (float*)ws : nullptr, (float*)(ws + l.edges), a->dgate, a->dpost_weight, a->dpost_bias,
+                       a->dnorm_weight, a->dnorm_bias, l.teams, l.rows_per_team};
+  return hip_status(launch_residual_norm_grad(a->dtype, n, s), "residual_norm_backward");
+}
+
+int triaccel_dropout(const triaccel_dropout_args* a, void* hip_stream) {
+  if (!a) return refuse(TRIACCEL_E_NULL_PTR, "args is NULL");
+  if (a->struct_size != sizeof(*a)) return refuse(TRIACCEL_E_INVALID_ARG, "struct_size");
+  TA_TRY(check_sizes(a->dtype, a->rows, a->cols, 1));
+  TA_TRY(check_drop(a->drop, a->scale));
+  TA_TRY(check_matrix(a->x, a->ldx, a->rows, a->cols, a->dtype, "x"));
+  if (a->residual) TA_TRY(check_matrix(a->residual, a->ldr, a->rows, a->cols, a->dtype, "residual"));
+  TA_TRY(check_matrix(a->y, a->ldy, a->rows, a->cols, a->dtype, "y"));
+  if (a->rows * ceil_div(a->cols, 512) > (int64_t)1 << 25) return refuse(TRIACCEL_E_INVALID_ARG, "dropout: more than 2^25 rows of 512 columns");
+  if (a->rows == 0) return TRIACCEL_OK;
+  const DropoutArgs d{a->rows, a->cols, a->x, a->residual, a->ldx, a->ldr, a->ldy, a->y};
+  return hip_status(launch_dropout(a->dtype, d, drop_of(a->drop, a->scale), (hipStream_t)hip_stream), "dropout");
+}
+
+}  // extern "C"

@@ -1,0 +1,151 @@
+// Row-wise layer kernels: gradients before an activation, sums over rows, dropout.  All are bound by memory.
+#include "layer_util.h"
+#include "layers.h"
+
+namespace triaccel {
+namespace layers {
+
+namespace {
+
+constexpr int kSlopeCols = 256, kSlopeLanes = kSlopeCols / 8, kSlopeRows = 256 / kSlopeLanes;
+
+// dz = s drop(dy) act'(pre), or dg = dh up act'(gate) and du = dh act(gate); with the sums of a block of rows per column.
+// A workgroup has 256 columns, 32 lanes of eight, and eight rows at a time.
+template <int DT, bool GATED>
+__global__ __launch_bounds__(256) void k_slope(SlopeArgs a, Drop drop) {
+  const int lane = threadIdx.x % kSlopeLanes, sub = threadIdx.x / kSlopeLanes;
+  const int64_t col = (int64_t)blockIdx.x * kSlopeCols + lane * 8, left = a.cols - col;
+  const int64_t r0 = (int64_t)blockIdx.y * a.rows_per_block;
+  const int64_t r1 = r0 + a.rows_per_block < a.rows ? r0 + a.rows_per_block : a.rows;
+  constexpr bool kExact = DT == kFP32;
+  constexpr int kSums = GATED ? 16 : 8;
+  float sum[kSums] = {};
+  if (col < a.width) {
+    DropKey key{};
+    if (!GATED && drop.limit) key = drop_key(drop);
+    for (int64_t r = r0 + sub; r < r1; r += kSlopeRows) {
+      float d[8], z[8];
+      load8<DT>(a.dy, r * a.lddy + col, left, d);
+      if constexpr (GATED) {
+        float u[8], du[8];
+        load8<DT>(a.gate, r * a.ldg + col, left, z);
+        load8<DT>(a.up, r * a.ldg + col, left, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float value, slope;
+          act_both<kExact>(a.act, z[i], value, slope);
+          const bool in = i < left;  // columns between cols and width are zeros
+          du[i] = in ? d[i] * value : 0.0f;
+          d[i] = in ? d[i] * u[i] * slope : 0.0f;
+          sum[i] += d[i];
+          sum[8 + i] += du[i];
+        }
+        if (a.dz) {
+          store8<DT>(a.dz, r * 2 * a.width + col, 8, d);
+          store8<DT>(a.dz, r * 2 * a.width + a.width + col, 8, du);
+        }
+      } else {
+        scale_drop8(drop, key, (uint64_t)r * (uint64_t)a.cols + (uint64_t)col, d);
+        if (a.act != kNone) {
+          load8<DT>(a.gate, r * a.ldg + col, left, z);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float value, slope;
+            act_both<kExact>(a.act, z[i], value, slope);
+            d[i] = i < left ? d[i] * slope : 0.0f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += d[i];
+        if (a.dz) store8<DT>(a.dz, r * a.width + col, 8, d);
+      }
+    }
+  }
+  if (!a.sums) return;
+  __shared__ float part[kSlopeRows][kSlopeCols + 4];
+#pragma unroll
+  for (int v = 0; v < kSums / 8; ++v) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[sub][lane * 8 + i] = sum[v * 8 + i];
+    __syncthreads();
+    float s = 0.0f;
+#pragma unroll
+    for (int r = 0; r < kSlopeRows; ++r) s += part[r][threadIdx.x];
+    const int64_t c = (int64_t)blockIdx.x * kSlopeCols + threadIdx.x;
+    if (c < a.cols) as_global<float>(a.sums)[((int64_t)blockIdx.y * (kSums / 8) + v) * a.cols + c] = s;
+    __syncthreads();
+  }
+}
+
+// 64 columns of one vector per workgroup, the blocks dealt to four wavefronts.
+__global__ __launch_bounds__(256) void k_column_sums(ColumnSums a) {
+  const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  void* out = a.out[blockIdx.y];
+  if (!out) return;
+  float s = 0.0f;
+  if (c < a.cols) {
+    const auto p = as_global<float>(a.sums) + (int64_t)blockIdx.y * a.cols + c;
+    for (int b = part; b < a.blocks; b += 4) s += p[(int64_t)b * a.stride];
+  }
+  __shared__ float all[4][64];
+  all[part][lane] = s;
+  __syncthreads();
+  if (part == 0 && c < a.cols) store1_of(a.dtype, out, c, (all[0][lane] + all[1][lane]) + (all[2][lane] + all[3][lane]));
+}
+
+// Eight elements per lane; a wavefront has 512 neighbouring columns of one row.
+template <int DT>
+__global__ __launch_bounds__(256) void k_dropout(DropoutArgs a, Drop drop, int64_t per_row) {
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int64_t row = wave / per_row, col = (wave - row * per_row) * 512 + (threadIdx.x & 63) * 8;
+  if (row >= a.rows || col >= a.cols) return;
+  const int64_t left = a.cols - col;
+  const DropKey key = drop_key(drop);
+  float v[8], r[8];
+  load8<DT>(a.x, row * a.ldx + col, left, v);
+  if (a.r) load8<DT>(a.r, row * a.ldr + col, left, r);
+  scale_drop8(drop, key, (uint64_t)row * (uint64_t)a.cols + (uint64_t)col, v);
+  if (a.r) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
+  }
+  store8<DT>(a.y, row * a.ldy + col, left, v);
+}
+
+}  // namespace
+
+hipError_t launch_slope(int dtype, bool gated, const SlopeArgs& a, hipStream_t stream) {
+  const dim3 grid((uint32_t)ceil_div(a.width, kSlopeCols), (uint32_t)a.blocks);
+  const Drop drop = a.drop ? *a.drop : Drop{0, 0, nullptr, 0, 1.0f};
+  const auto go = [&](auto dt) {
+    constexpr int DT = decltype(dt)::value;
+    if (gated) k_slope<DT, true><<<grid, 256, 0, stream>>>(a, drop);
+    else k_slope<DT, false><<<grid, 256, 0, stream>>>(a, drop);
+  };
+  if (dtype == kFP16) go(std::integral_constant<int, kFP16>());
+  else if (dtype == kBF16) go(std::integral_constant<int, kBF16>());
+  else go(std::integral_constant<int, kFP32>());
+  return hipGetLastError();
+}
+
+hipError_t launch_column_sums(const ColumnSums& a, hipStream_t stream) {
+  k_column_sums<<<dim3((uint32_t)ceil_div(a.cols, 64), (uint32_t)a.vectors), 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_dropout(int dtype, const DropoutArgs& in, const Drop& d, hipStream_t stream) {
+  DropoutArgs a = in;
+  if (a.ldx == a.cols && a.ldy == a.cols && (!a.r || a.ldr == a.cols)) {  // one long row: the same elements have the same numbers
+    a.cols *= a.rows;
+    a.rows = 1;
+  }
+  const int64_t per_row = ceil_div(a.cols, 512), groups = ceil_div(a.rows * per_row, 4);
+  if (dtype == kFP16) k_dropout<kFP16><<<dim3((uint32_t)groups), 256, 0, stream>>>(a, d, per_row);
+  else if (dtype == kBF16) k_dropout<kBF16><<<dim3((uint32_t)groups), 256, 0, stream>>>(a, d, per_row);
+  else k_dropout<kFP32><<<dim3((uint32_t)groups), 256, 0, stream>>>(a, d, per_row);
+  return hipGetLastError();
+}
+
+}  // namespace layers
+}  // namespace triaccel

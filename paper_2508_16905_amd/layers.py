@@ -1,0 +1,354 @@
+"""The layer operators of a feed-forward block on PyTorch-ROCm tensors: addresses, strides and streams are handed to the C ABI
+of ``include/triaccel_layers.h``, outputs and workspaces are allocated, and nothing is computed here.
+
+    linear         y = r + s drop(act(x W^T + b))
+    gated          h = act(x Wg^T + bg) * (x Wu^T + bu)
+    residual_norm  r' = r + s g * P(b), y = N(r')
+    dropout        y = r + s drop(x)
+
+Each has its gradients as a call of its own: the optimizer step takes gradients as flat tensors, and nothing between the two
+needs a graph of the computation.  ``act`` is "none", "relu", "silu", "gelu" or "gelu_tanh".
+
+A matrix has any number of leading dimensions, which are its rows, and a last dimension of stride 1; rows may lie apart (a
+view of some columns).  All matrices of a call have one type, float16, bfloat16 or float32; vectors may have another.  Work is
+enqueued on the current stream of the tensors' device, and nothing is synchronised.
+"""
+
+from __future__ import annotations
+
+import ctypes as C
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import binding as B
+
+_CODE = {torch.float16: B.FP16, torch.bfloat16: B.BF16, torch.float32: B.FP32}
+_ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+_KIND = {"rms": 1, "layer": 2}
+
+
+class Dropout(NamedTuple):
+    """Elements are dropped with probability ``p`` (rounded to 1/65536).  ``seed`` and ``offset`` name the mask: the same pair
+    gives the same mask in the backward pass.  ``state``, an int64 tensor (seed, offset) on the device, takes their place where
+    a captured graph is to draw another mask at each replay."""
+
+    p: float
+    seed: int = 0
+    offset: int = 0
+    state: Optional[torch.Tensor] = None
+
+
+class Norm(NamedTuple):
+    """``kind``: "rms" or "layer"; no weight means ones, no bias zeros."""
+
+    kind: str
+    weight: Optional[torch.Tensor] = None
+    bias: Optional[torch.Tensor] = None
+    eps: float = 1e-6
+
+
+class ResidualNormGrads(NamedTuple):
+    residual: Optional[torch.Tensor]
+    block: Optional[torch.Tensor]
+    gate: Optional[torch.Tensor]
+    post_weight: Optional[torch.Tensor]
+    post_bias: Optional[torch.Tensor]
+    norm_weight: Optional[torch.Tensor]
+    norm_bias: Optional[torch.Tensor]
+
+
+def _refuse(name: str, why: str):
+    raise ValueError(f"{name}: {why}")
+
+
+def _matrix(t: torch.Tensor, name: str, cols: int = 0, like: Optional[torch.Tensor] = None, rows: int = -1):
+    """(address, row stride, rows, columns) of a matrix."""
+    if not t.is_cuda:
+        _refuse(name, "a tensor on the GPU is wanted")
+    if t.dtype not in _CODE:
+        _refuse(name, f"float16, bfloat16 or float32 is wanted, not {t.dtype}")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        _refuse(name, f"type or device differs from the call's ({like.dtype}, {like.device})")
+    dim = t.dim()
+    if dim == 0 or t.shape[-1] == 0:
+        _refuse(name, "at least one column is wanted")
+    n = t.shape[-1]
+    if cols and n != cols:
+        _refuse(name, f"{n} columns where the call has {cols}")
+    if dim == 2:
+        m, ld = t.shape[0], t.stride(0)
+    elif dim == 1:
+        m, ld = 1, n
+    else:
+        m, ld, step = t.numel() // n, 0, 0
+        if m:
+            for i in range(dim - 2, -1, -1):   # the leading dimensions have to be one run of rows
+                if t.shape[i] > 1:
+                    if ld == 0:
+                        ld = step = t.stride(i)
+                    elif t.stride(i) != step:
+                        _refuse(name, "the leading dimensions do not lie one after another: make it contiguous")
+                    step *= t.shape[i]
+    if rows >= 0 and m != rows:
+        _refuse(name, f"{m} rows where the call has {rows}")
+    if n > 1 and t.stride(-1) != 1:
+        _refuse(name, "the last dimension has to have stride 1")
+    if m <= 1:
+        ld = n
+    if ld < n:
+        _refuse(name, "rows overlap (an expanded tensor): make it contiguous")
+    return t.data_ptr(), ld, m, n
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int, like: torch.Tensor):
+    """(address, precision code) of a vector; (None, FP32) if there is none."""
+    if t is None:
+        return None, B.FP32
+    if t.dtype not in _CODE or t.device != like.device:
+        _refuse(name, "float16, bfloat16 or float32 on the call's device is wanted")
+    if t.numel() != n or not t.is_contiguous():
+        _refuse(name, f"{n} contiguous values are wanted")
+    return t.data_ptr(), _CODE[t.dtype]
+
+
+def _drop(d: Optional[Dropout], like: torch.Tensor):
+    if d is None:
+        return B.DropoutSpec(0.0, 0, 0, None)
+    if d.state is None:
+        return B.DropoutSpec(d.p, d.seed & 0xFFFFFFFFFFFFFFFF, d.offset & 0xFFFFFFFFFFFFFFFF, None)
+    if d.state.dtype != torch.int64 or d.state.numel() != 2 or not d.state.is_contiguous() or d.state.device != like.device:
+        _refuse("dropout", "state is an int64 tensor of two values on the call's device")
+    return B.DropoutSpec(d.p, 0, 0, d.state.data_ptr())
+
+
+def _act(name: str) -> int:
+    if name not in _ACT:
+        _refuse("act", f"one of {', '.join(_ACT)} is wanted, not {name!r}")
+    return _ACT[name]
+
+
+def _call(name: str, args, like: torch.Tensor):
+    lib = B._lib or B.load_library()
+    workspace = getattr(lib, name + "_workspace", None) if B._LAYER_CALLS[name][1] else None
+    with _On(like.device):
+        keep = None
+        if workspace is not None:
+            size = workspace(C.byref(args))
+            if size < 0:
+                raise B.TriAccelError(int(size), name)
+            if size:
+                keep = torch.empty(size, dtype=torch.uint8, device=like.device)
+                args.workspace, args.workspace_bytes = keep.data_ptr(), size
+        code = getattr(lib, name)(C.byref(args), torch.cuda.current_stream(like.device).cuda_stream)
+    if code != 0:
+        raise B.TriAccelError(code, name)
+
+
+class _On:
+    """The tensors' device as the current one, where it is not already."""
+
+    __slots__ = ("at", "before")
+
+    def __init__(self, device):
+        self.at, self.before = device.index, None
+
+    def __enter__(self):
+        now = torch.cuda.current_device()
+        if now != self.at:
+            self.before = now
+            torch.cuda.set_device(self.at)
+
+    def __exit__(self, *_):
+        if self.before is not None:
+            torch.cuda.set_device(self.before)
+
+
+def _new(like: torch.Tensor, cols: int) -> torch.Tensor:
+    """A dense matrix of the leading dimensions of ``like``."""
+    return torch.empty(*like.shape[:-1], cols, dtype=like.dtype, device=like.device)
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+           act: str = "none", scale: float = 1.0, dropout: Optional[Dropout] = None, save: bool = False,
+           out: Optional[torch.Tensor] = None):
+    """r + scale * drop(act(x W^T + b)) with x (..., in) and W (out, in).  ``save``: returns (y, x W^T + b) instead of y, the second
+    for ``linear_backward``.  ``out``: where y goes; it may be the residual."""
+    px, ldx, rows, k = _matrix(x, "x")
+    pw, ldw, n, _ = _matrix(weight, "weight", k, x)
+    pb, bias_code = _vector(bias, "bias", n, x)
+    pr, ldr = _matrix(residual, "residual", n, x, rows)[:2] if residual is not None else (None, 0)
+    y = _new(x, n) if out is None else out
+    py, ldy = _matrix(y, "out", n, x, rows)[:2]
+    pre = _new(x, n) if save else None
+    args = B.LinearArgs(C.sizeof(B.LinearArgs), _CODE[x.dtype], rows, k, n, px, ldx, pw, ldw, pb, pr, ldr, py, ldy,
+                        pre.data_ptr() if save else None, n, bias_code, _act(act), scale, 0, _drop(dropout, x), None, 0)
+    _call("triaccel_linear", args, x)
+    return (y, pre) if save else y
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre: Optional[torch.Tensor] = None, act: str = "none",
+                    scale: float = 1.0, dropout: Optional[Dropout] = None, x_grad: bool = True, weight_grad: bool = True,
+                    bias_grad: bool = False, weight_grad_dtype: Optional[torch.dtype] = None):
+    """(dx, dW, db), None where not asked for.  ``act``, ``scale`` and ``dropout`` as in the forward call, ``pre`` what it kept
+    (not needed for act "none").  dW has the type of the call, or float32; db is float32.  The gradient of the residual is dy."""
+    pd, lddy, rows, n = _matrix(dy, "dy")
+    px, ldx, _, k = _matrix(x, "x", 0, dy, rows)
+    pw, ldw = _matrix(weight, "weight", k, dy, n)[:2]
+    code = _act(act)
+    if code and pre is None:
+        _refuse("pre", "the value before the activation is needed")
+    pp, ldp = _matrix(pre, "pre", n, dy, rows)[:2] if code else (None, 0)
+    dx = _new(x, k) if x_grad else None
+    dw = torch.empty(n, k, dtype=weight_grad_dtype or dy.dtype, device=dy.device) if weight_grad else None
+    db = torch.empty(n, dtype=torch.float32, device=dy.device) if bias_grad else None
+    if dw is not None and dw.dtype not in (dy.dtype, torch.float32):
+        _refuse("weight_grad_dtype", "the type of the call or float32 is wanted")
+    args = B.LinearBackwardArgs(C.sizeof(B.LinearBackwardArgs), _CODE[dy.dtype], rows, k, n, pd, lddy, px, ldx, pw, ldw, pp, ldp,
+                                dx.data_ptr() if x_grad else None, k, dw.data_ptr() if weight_grad else None, k,
+                                db.data_ptr() if bias_grad else None, _CODE[dw.dtype] if weight_grad else B.FP32, B.FP32, code, scale,
+                                _drop(dropout, dy), None, 0)
+    _call("triaccel_linear_backward", args, dy)
+    return dx, dw, db
+
+
+def gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Optional[torch.Tensor] = None,
+          b_up: Optional[torch.Tensor] = None, act: str = "silu", save: bool = False):
+    """act(x Wg^T + bg) * (x Wu^T + bu), both products in one kernel.  ``save``: returns (h, gate, up), the latter two (before the
+    activation) for ``gated_backward``."""
+    px, ldx, rows, k = _matrix(x, "x")
+    pg, ldw, n, _ = _matrix(w_gate, "w_gate", k, x)
+    pu, ldu = _matrix(w_up, "w_up", k, x, n)[:2]
+    if ldw != ldu:
+        _refuse("w_up", "its row stride differs from w_gate's")
+    bg, bias_code = _vector(b_gate, "b_gate", n, x)
+    bu, up_code = _vector(b_up, "b_up", n, x)
+    if (bg is None) != (bu is None) or bias_code != up_code:
+        _refuse("b_up", "both biases, of one type, or none")
+    h = _new(x, n)
+    g, u = (_new(x, n), _new(x, n)) if save else (None, None)
+    args = B.GatedArgs(C.sizeof(B.GatedArgs), _CODE[x.dtype], rows, k, n, px, ldx, pg, pu, ldw, bg, bu, h.data_ptr(), n,
+                       g.data_ptr() if save else None, u.data_ptr() if save else None, n, bias_code, _act(act), None, 0)
+    _call("triaccel_gated", args, x)
+    return (h, g, u) if save else h
+
+
+def gated_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, gate: torch.Tensor, up: torch.Tensor,
+                   act: str = "silu", x_grad: bool = True, weight_grad: bool = True, bias_grad: bool = False,
+                   weight_grad_dtype: Optional[torch.dtype] = None):
+    """(dx, dWg, dWu, dbg, dbu), None where not asked for; ``gate`` and ``up`` are what the forward call kept."""
+    pd, lddh, rows, n = _matrix(dh, "dh")
+    px, ldx, _, k = _matrix(x, "x", 0, dh, rows)
+    pg, ldw = _matrix(w_gate, "w_gate", k, dh, n)[:2]
+    pu, ldu = _matrix(w_up, "w_up", k, dh, n)[:2]
+    if ldw != ldu:
+        _refuse("w_up", "its row stride differs from w_gate's")
+    qg, ldg = _matrix(gate, "gate", n, dh, rows)[:2]
+    qu, ldq = _matrix(up, "up", n, dh, rows)[:2]
+    if ldg != ldq:
+        _refuse("up", "its row stride differs from gate's")
+    dt = weight_grad_dtype or dh.dtype
+    if dt not in (dh.dtype, torch.float32):
+        _refuse("weight_grad_dtype", "the type of the call or float32 is wanted")
+    dx = _new(x, k) if x_grad else None
+    dwg, dwu = (torch.empty(n, k, dtype=dt, device=dh.device), torch.empty(n, k, dtype=dt, device=dh.device)) if weight_grad else (None, None)
+    dbg, dbu = (torch.empty(n, device=dh.device), torch.empty(n, device=dh.device)) if bias_grad else (None, None)
+    args = B.GatedBackwardArgs(C.sizeof(B.GatedBackwardArgs), _CODE[dh.dtype], rows, k, n, pd, lddh, px, ldx, pg, pu, ldw, qg, qu, ldg,
+                               dx.data_ptr() if x_grad else None, k, dwg.data_ptr() if weight_grad else None,
+                               dwu.data_ptr() if weight_grad else None, k, dbg.data_ptr() if bias_grad else None,
+                               dbu.data_ptr() if bias_grad else None, _CODE[dt], B.FP32, _act(act), 0, None, 0)
+    _call("triaccel_gated_backward", args, dh)
+    return dx, dwg, dwu, dbg, dbu
+
+
+def _norm_spec(n: Optional[Norm], name: str, cols: int, like: torch.Tensor) -> B.NormSpec:
+    if n is None:
+        return B.NormSpec(0, B.FP32, None, None, 0.0, 0)
+    if n.kind not in _KIND:
+        _refuse(name, f"kind is rms or layer, not {n.kind!r}")
+    pw, cw = _vector(n.weight, name + " weight", cols, like)
+    pb, cb = _vector(n.bias, name + " bias", cols, like)
+    if pw is not None and pb is not None and cw != cb:
+        _refuse(name, "weight and bias have different types")
+    return B.NormSpec(_KIND[n.kind], cw if pw is not None else cb, pw, pb, n.eps, 0)
+
+
+def _gate(gate: Optional[torch.Tensor], rows_per_gate: int, rows: int, cols: int, like: torch.Tensor):
+    if gate is None:
+        return None, 0, B.FP32
+    if rows_per_gate == 0:
+        p, code = _vector(gate, "gate", cols, like)
+        return p, cols, code
+    if rows_per_gate < 0:
+        _refuse("rows_per_gate", "0, or the rows that share a row of the gate")
+    if gate.device != like.device or gate.dim() != 2 or gate.shape[0] < -(-rows // rows_per_gate):
+        _refuse("gate", "a matrix with a row for each rows_per_gate rows is wanted, on the call's device")
+    p, ld = _matrix(gate, "gate", cols)[:2]
+    return p, ld, _CODE[gate.dtype]
+
+
+def residual_norm(residual: torch.Tensor, block: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0,
+                  post: Optional[Norm] = None, norm: Optional[Norm] = None, scale: float = 1.0):
+    """r' = r + scale * gate * post(block) and y = norm(r'): returns (r', y).  Without a block r' is the residual itself, without
+    a norm y is None.  ``gate``: one vector, or with ``rows_per_gate`` a matrix whose row i stands for that many rows from
+    ``i * rows_per_gate`` on (a condition per sequence)."""
+    pr, ldr, rows, n = _matrix(residual, "residual")
+    pb, ldb = _matrix(block, "block", n, residual, rows)[:2] if block is not None else (None, n)
+    pg, ldg, gate_code = _gate(gate, rows_per_gate, rows, n, residual)
+    out = _new(residual, n) if block is not None else residual
+    y = _new(residual, n) if norm is not None else None
+    args = B.ResidualNormArgs(C.sizeof(B.ResidualNormArgs), _CODE[residual.dtype], rows, n, pr, ldr, pb, ldb, pg, ldg, rows_per_gate,
+                              out.data_ptr() if block is not None else None, n, y.data_ptr() if norm is not None else None, n, gate_code, scale,
+                              _norm_spec(post, "post", n, residual), _norm_spec(norm, "norm", n, residual))
+    _call("triaccel_residual_norm", args, residual)
+    return out, y
+
+
+def residual_norm_backward(dresidual: Optional[torch.Tensor], dy: Optional[torch.Tensor], residual: torch.Tensor,
+                           block: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0,
+                           post: Optional[Norm] = None, norm: Optional[Norm] = None, scale: float = 1.0) -> ResidualNormGrads:
+    """Gradients from those of r' (``dresidual``, None = 0) and of y (``dy``, None = 0); ``residual`` is the r' that the forward call
+    returned, the rest as it was given.  Vectors' gradients are float32, one for each weight, bias and gate that was given."""
+    pr, ldr, rows, n = _matrix(residual, "residual")
+    like = residual
+    pd, ldd = _matrix(dresidual, "dresidual", n, like, rows)[:2] if dresidual is not None else (None, n)
+    py, ldy = _matrix(dy, "dy", n, like, rows)[:2] if dy is not None else (None, n)
+    pb, ldb = _matrix(block, "block", n, like, rows)[:2] if block is not None else (None, n)
+    if block is None and (gate is not None or post is not None):
+        _refuse("block", "a gate or a norm after the block without a block")
+    pg, ldg, gate_code = _gate(gate, rows_per_gate, rows, n, like)
+    post_spec, norm_spec = _norm_spec(post, "post", n, like), _norm_spec(norm, "norm", n, like)
+
+    def vector(t):
+        return None if t is None else torch.empty(n, dtype=torch.float32, device=like.device)
+
+    def at(t):
+        return None if t is None else t.data_ptr()
+
+    groups = -(-rows // rows_per_gate) if rows_per_gate else 1
+    dgate = None if gate is None else torch.empty((groups, n) if rows_per_gate else n, dtype=torch.float32, device=like.device)
+    dpw, dpb = (vector(post.weight), vector(post.bias)) if post is not None else (None, None)
+    dnw, dnb = (vector(norm.weight), vector(norm.bias)) if norm is not None else (None, None)
+    dr, db = _new(like, n), _new(like, n) if block is not None else None
+    args = B.ResidualNormBackwardArgs(C.sizeof(B.ResidualNormBackwardArgs), _CODE[like.dtype], rows, n, pd, ldd, py, ldy, pr, ldr, pb, ldb,
+                                      pg, ldg, rows_per_gate, dr.data_ptr(), n, at(db), n, at(dgate), at(dpw), at(dpb), at(dnw), at(dnb),
+                                      gate_code, B.FP32, scale, 0, post_spec, norm_spec, None, 0)
+    _call("triaccel_residual_norm_backward", args, like)
+    return ResidualNormGrads(dr, db, dgate, dpw, dpb, dnw, dnb)
+
+
+def dropout(x: torch.Tensor, drop: Dropout, residual: Optional[torch.Tensor] = None, scale: float = 1.0,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """r + scale * drop(x)."""
+    px, ldx, rows, n = _matrix(x, "x")
+    pr, ldr = _matrix(residual, "residual", n, x, rows)[:2] if residual is not None else (None, n)
+    y = _new(x, n) if out is None else out
+    py, ldy = _matrix(y, "out", n, x, rows)[:2]
+    args = B.DropoutArgs(C.sizeof(B.DropoutArgs), _CODE[x.dtype], rows, n, px, ldx, pr, ldr, py, ldy, scale, 0, _drop(drop, x))
+    _call("triaccel_dropout", args, x)
+    return y
+
+
+def dropout_backward(dy: torch.Tensor, drop: Dropout, scale: float = 1.0) -> torch.Tensor:
+    """The gradient of x in ``dropout``: the same mask and scale on dy.  The gradient of the residual is dy."""
+    return dropout(dy, drop, scale=scale)
