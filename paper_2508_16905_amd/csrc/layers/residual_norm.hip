@@ -1,6 +1,7 @@
 // r' = r + s g * P(b), y = N(r') and its gradients: one pass over the rows, a row in the registers of a team of lanes.
 // Bound by memory: forward reads r and b and writes r' and y, backward reads dr', dy, r' and b and writes dr and db.  All
 // sums are fp32; the statistics of the backward pass are computed again from the rows that it reads anyway.
+#include "../device_util.h"
 #include "layer_util.h"
 #include "layers.h"
 
@@ -14,9 +15,16 @@ namespace {
 template <int N>
 __device__ __forceinline__ void wave_sum(float (&v)[N]) {
 #pragma unroll
-  for (int s = 32; s > 0; s >>= 1) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], s, 64);
+  for (int i = 0; i < N; ++i) {
+    const auto add = [](float x, uint32_t y) { return x + u2f(y); };
+    float x = v[i];
+    x = add(x, TA_DPP(f2u(x), 0x111, 0xF));
+    x = add(x, TA_DPP(f2u(x), 0x112, 0xF));
+    x = add(x, TA_DPP(f2u(x), 0x114, 0xF));
+    x = add(x, TA_DPP(f2u(x), 0x118, 0xF));
+    x = add(x, TA_DPP(f2u(x), 0x142, 0xA));
+    x = add(x, TA_DPP(f2u(x), 0x143, 0xC));
+    v[i] = u2f(last_lane(f2u(x)));
   }
 }
 template <int T, int N>
@@ -24,18 +32,18 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float* lds, int& turn) {
   wave_sum(v);
   if constexpr (T > 64) {
     constexpr int kWaves = T / 64;
-    float* place = lds + turn * (4 * kWaves);
+    float* place = lds + turn * (2 * kWaves);
     turn ^= 1;
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) place[(threadIdx.x >> 6) * 4 + i] = v[i];
+      for (int i = 0; i < N; ++i) place[i * kWaves + (threadIdx.x >> 6)] = v[i];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float s = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) s += place[w * 4 + i];
+      for (int w = 0; w < kWaves; ++w) s += place[i * kWaves + w];
       v[i] = s;
     }
   }
@@ -79,7 +87,7 @@ __device__ __forceinline__ void vector8(const void* p, int dtype, int64_t col, i
 template <int DT, int T, int V>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void k_residual_norm(NormArgs a) {
   constexpr int kThreads = T < 256 ? 256 : T, kTeams = kThreads / T;
-  __shared__ float lds[2 * 4 * (kThreads / 64)];
+  __shared__ float lds[2 * 2 * (kThreads / 64)];
   const int lane = threadIdx.x % T;
   const int64_t row = (int64_t)blockIdx.x * kTeams + threadIdx.x / T;
   if (kTeams > 1 && row >= a.rows) return;  // a wavefront of its own: nobody waits for it
@@ -138,84 +146,169 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_residual_norm(NormArgs a)
   }
 }
 
-// A team has a run of rows and keeps its columns' sums for the vectors' gradients in registers; a second kernel adds up the
-// teams.  A gate with a row for each `rows_per_gate` rows is written where the team has all of these, and left in one of two
-// places of the team (the group it begins in, another) where it has a part.
-template <int DT, int T, int V>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void k_residual_norm_grad(NormGradArgs a) {
-  constexpr int kThreads = T < 256 ? 256 : T, kTeams = kThreads / T;
-  __shared__ float lds[2 * 4 * (kThreads / 64)];
-  const int lane = threadIdx.x % T;
-  const int64_t team = (int64_t)blockIdx.x * kTeams + threadIdx.x / T;
-  if (kTeams > 1 && team >= a.teams) return;
+// A team of T lanes, V groups of eight columns each, has a run of rows and keeps its columns' sums for the vectors' gradients
+// in registers; k_norm_vectors adds up the teams.  A gate with a row for each `rows_per_gate` rows is written where the team
+// has all of these, and left in one of two places of the team (the group it begins in, another) where it has a part.
+//
+// Bound by memory once the arithmetic is kept out of its way (about 45 operations an element; at 8192 x 4096 in bf16 this is as
+// long as the reading and writing): the next row is loaded before this one is worked on, the vectors stay in
+// LDS (V = 1; in registers they would leave room for half as many wavefronts), and rows that fill their lanes (FULL) go without
+// a test per element.
+template <int DT, int T, int V, bool FULL>
+__global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual_norm_grad(NormGradArgs a) {
+  constexpr bool kKeep = V == 1;
+  __shared__ float lds[2 * 2 * (T / 64)];
+  __shared__ f32x4 kept[kKeep ? 8 * T : 1];  // a lane reads only what it wrote
+  const int lane = threadIdx.x;
+  const int64_t team = blockIdx.x;
   const int64_t r0 = team * a.rows_per_team, r1 = r0 + a.rows_per_team < a.rows ? r0 + a.rows_per_team : a.rows;
   int turn = 0;
   const float cols = (float)a.cols, inv = 1.0f / cols;
-  const bool post = a.b && a.post.kind;
-  int64_t col[V], left[V];
-  bool in[V];
-  float nw[V][8], nb[V][8], pw[V][8], pb[V][8], gs[V][8];
+  const bool next = a.norm.kind && a.dy, post = a.b && a.post.kind, next_centred = a.norm.kind == 2, post_centred = a.post.kind == 2;
+  int col[V], left[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    col[v] = ((int64_t)v * T + lane) * 8;
-    left[v] = a.cols - col[v];
-    in[v] = left[v] > 0;
+    col[v] = (v * T + lane) * 8;
+    left[v] = FULL ? 8 : (int)a.cols - col[v];
+  }
+  const auto live = [&](int v, int i) { return FULL || i < left[v]; };
+  // vectors of this lane's columns; zeros past the end
+  const auto vector = [&](const void* p, int dtype, int64_t at, int v, float otherwise, float (&out)[8]) {
+    if (p) {
+      load8_of(dtype, p, at + col[v], left[v], out);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) out[i] = live(v, i) ? otherwise : 0.0f;
+    }
+  };
+  float nw[V][8], nb[V][8], pw[V][8], pb[V][8], gs[V][8];
+#pragma unroll
+  for (int v = 0; v < V; ++v)
 #pragma unroll
     for (int i = 0; i < 8; ++i) nw[v][i] = nb[v][i] = pw[v][i] = pb[v][i] = gs[v][i] = 0.0f;
+  const auto keep = [&](int which, const float (&x)[8]) {
+    kept[2 * which * T + lane] = f32x4{x[0], x[1], x[2], x[3]};
+    kept[(2 * which + 1) * T + lane] = f32x4{x[4], x[5], x[6], x[7]};
+  };
+  const auto recall = [&](int which, float (&x)[8]) {
+    *(f32x4*)x = kept[2 * which * T + lane];
+    *(f32x4*)(x + 4) = kept[(2 * which + 1) * T + lane];
+  };
+  const auto norm_weight = [&](int v, float (&x)[8]) { vector(a.norm.weight, a.norm.dtype, 0, v, 1.0f, x); };
+  const auto post_weight = [&](int v, float (&x)[8]) { vector(a.post.weight, a.post.dtype, 0, v, 1.0f, x); };
+  const auto post_bias = [&](int v, float (&x)[8]) { vector(a.post.bias, a.post.dtype, 0, v, 0.0f, x); };
+  if constexpr (kKeep) {
+    float x[8];
+    norm_weight(0, x);
+    keep(0, x);
+    post_weight(0, x);
+    keep(1, x);
+    post_bias(0, x);
+    keep(2, x);
   }
-  int64_t group = a.rows_per_gate ? r0 / a.rows_per_gate : 0;
+  int64_t group = a.rows_per_gate ? r0 / a.rows_per_gate : 0, group_end = a.rows_per_gate ? (group + 1) * a.rows_per_gate : a.rows;
   const int64_t first_group = group;
-  const auto flush_gate = [&](int64_t g) {
-    const int64_t g0 = g * a.rows_per_gate, g1 = g0 + a.rows_per_gate < a.rows ? g0 + a.rows_per_gate : a.rows;
+  const auto scaled_gate = [&](int v, float (&x)[8]) {
+    vector(a.gate, a.gate_dtype, a.rows_per_gate ? group * a.ldgate : 0, v, 1.0f, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= a.scale;
+  };
+  const auto keep_gate = [&]() {
+    if constexpr (kKeep) {
+      float x[8];
+      scaled_gate(0, x);
+      keep(3, x);
+    }
+  };
+  keep_gate();
+  const auto flush_gate = [&]() {
+    const int64_t g0 = group * a.rows_per_gate, g1 = g0 + a.rows_per_gate < a.rows ? g0 + a.rows_per_gate : a.rows;
     const bool whole = g0 >= r0 && g1 <= r1;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      if (in[v]) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (i < left[v]) {
-            if (whole) store1_of(a.vec_dtype, a.dgate, g * a.cols + col[v] + i, gs[v][i]);
-            else as_global<float>(a.gate_edges)[(team * 2 + (g == first_group ? 0 : 1)) * a.cols + col[v] + i] = gs[v][i];
-          }
+      for (int i = 0; i < 8; ++i) {
+        if (live(v, i)) {
+          const float s = a.scale * gs[v][i];
+          if (whole) store1_of(a.vec_dtype, a.dgate, group * a.cols + col[v] + i, s);
+          else as_global<float>(a.gate_edges)[(team * 2 + (group == first_group ? 0 : 1)) * a.cols + col[v] + i] = s;
         }
+        gs[v][i] = 0.0f;
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) gs[v][i] = 0.0f;
     }
   };
-  for (int64_t row = r0; row < r1; ++row) {
-    if (a.rows_per_gate && a.dgate) {
-      const int64_t g = row / a.rows_per_gate;
-      if (g != group) {
-        flush_gate(group);
-        group = g;
-      }
-    }
-    float d[V][8], r[V][8], dy[V][8];
+  Elem8<DT> q_d[V], q_dy[V], q_r[V], q_b[V];
+  const auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) d[v][i] = r[v][i] = dy[v][i] = 0.0f;
-      if (in[v]) {
-        if (a.dro) load8<DT>(a.dro, row * a.lddro + col[v], left[v], d[v]);
-        if (a.norm.kind && a.dy) {
-          load8<DT>(a.dy, row * a.lddy + col[v], left[v], dy[v]);
-          load8<DT>(a.r, row * a.ldr + col[v], left[v], r[v]);
-        }
-      }
+      const auto get = [&](const void* p, int64_t ld) {
+        return load_raw8<DT>((const Elem<DT>*)p + row * ld + col[v], p ? left[v] : 0);
+      };
+      q_d[v] = get(a.dro, a.lddro);
+      q_dy[v] = get(next ? a.dy : nullptr, a.lddy);
+      q_r[v] = get(next ? a.r : nullptr, a.ldr);
+      q_b[v] = get(a.b, a.ldb);
     }
-    if (a.norm.kind && a.dy) {
-      float mean, rstd;
-      statistics<T, V>(a.norm.kind, r, in, left, cols, a.norm.eps, lds, turn, mean, rstd);
+  };
+  fetch(r0);
+  for (int64_t row = r0; row < r1; ++row) {
+    if (row == group_end) {
+      if (a.dgate) flush_gate();
+      ++group;
+      group_end += a.rows_per_gate;
+      keep_gate();
+    }
+    float d[V][8], r[V][8], dy[V][8], b[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[v][i] = (float)q_d[v][i];
+        dy[v][i] = (float)q_dy[v][i];
+        r[v][i] = (float)q_r[v][i];
+        b[v][i] = (float)q_b[v][i];
+      }
+    if (row + 1 < r1) fetch(row + 1);
+    // both rows' statistics: means, then sums of squares around them
+    float rstd = 0.0f, brstd = 1.0f;
+    {
+      float mean[2] = {0.0f, 0.0f};
+      if ((next && next_centred) || (post && post_centred)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            mean[0] += r[v][i];
+            mean[1] += b[v][i];
+          }
+        team_sum<T>(mean, lds, turn);
+        mean[0] = next_centred ? mean[0] * inv : 0.0f;
+        mean[1] = post && post_centred ? mean[1] * inv : 0.0f;
+      }
+      float sq[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (next) r[v][i] = live(v, i) ? r[v][i] - mean[0] : 0.0f;
+          if (post) b[v][i] = live(v, i) ? b[v][i] - mean[1] : 0.0f;
+          sq[0] = fmaf(r[v][i], r[v][i], sq[0]);
+          sq[1] = fmaf(b[v][i], b[v][i], sq[1]);
+        }
+      if (next || post) team_sum<T>(sq, lds, turn);
+      if (next) rstd = 1.0f / sqrtf(sq[0] / cols + a.norm.eps);
+      if (post) brstd = 1.0f / sqrtf(sq[1] / cols + a.post.eps);
+    }
+    if (next) {
       float s[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         float w[8];
-        if (in[v]) vector8(a.norm.weight, a.norm.dtype, col[v], left[v], 1.0f, w);
+        if constexpr (kKeep) recall(0, w);
+        else norm_weight(v, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (!in[v] || i >= left[v]) continue;
-          r[v][i] = (r[v][i] - mean) * rstd;
+          r[v][i] *= rstd;
           nw[v][i] = fmaf(dy[v][i], r[v][i], nw[v][i]);
           nb[v][i] += dy[v][i];
           dy[v][i] *= w[i];
@@ -224,47 +317,38 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_residual_norm_grad(NormGr
         }
       }
       team_sum<T>(s, lds, turn);
-      const float along = s[0] * inv, centre = a.norm.kind == 2 ? s[1] * inv : 0.0f;
+      const float along = s[0] * inv, centre = next_centred ? s[1] * inv : 0.0f;
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (in[v] && i < left[v]) d[v][i] = fmaf(rstd, dy[v][i] - centre - r[v][i] * along, d[v][i]);
+        for (int i = 0; i < 8; ++i) d[v][i] = fmaf(rstd, fmaf(-along, r[v][i], dy[v][i] - centre), d[v][i]);
     }
+    if (a.dr) {
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (in[v] && a.dr) store8<DT>(a.dr, row * a.lddr + col[v], left[v], d[v]);
+      for (int v = 0; v < V; ++v) store8<DT>(a.dr, row * a.lddr + col[v], left[v], d[v]);
+    }
     if (!a.b) continue;
     // the block's side: t = P(b), dP = s g d
-    float b[V][8], g[V][8];
-    const int64_t gate_row = a.rows_per_gate ? row / a.rows_per_gate * a.ldgate : 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) b[v][i] = g[v][i] = 0.0f;
-      if (in[v]) {
-        if (a.b) load8<DT>(a.b, row * a.ldb + col[v], left[v], b[v]);
-        vector8(a.gate, a.gate_dtype, gate_row + col[v], left[v], 1.0f, g[v]);
-      }
-    }
-    float rstd = 1.0f, along = 0.0f, centre = 0.0f;
     if (post) {
-      float mean;
-      statistics<T, V>(a.post.kind, b, in, left, cols, a.post.eps, lds, turn, mean, rstd);
       float s[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float w[8], c[8];
-        if (in[v]) {
-          vector8(a.post.weight, a.post.dtype, col[v], left[v], 1.0f, w);
-          vector8(a.post.bias, a.post.dtype, col[v], left[v], 0.0f, c);
+        float w[8], c[8], g[8];
+        if constexpr (kKeep) {
+          recall(1, w);
+          recall(2, c);
+          recall(3, g);
+        } else {
+          post_weight(v, w);
+          post_bias(v, c);
+          scaled_gate(v, g);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (!in[v] || i >= left[v]) continue;
-          b[v][i] = (b[v][i] - mean) * rstd;
-          const float t = fmaf(b[v][i], w[i], c[i]), dp = a.scale * g[v][i] * d[v][i];
-          gs[v][i] = fmaf(a.scale * d[v][i], t, gs[v][i]);
+          b[v][i] *= brstd;
+          gs[v][i] = fmaf(d[v][i], fmaf(b[v][i], w[i], c[i]), gs[v][i]);
+          // past the end the factor is 0, whatever d became there
+          const float dp = g[i] * d[v][i];
           pw[v][i] = fmaf(dp, b[v][i], pw[v][i]);
           pb[v][i] += dp;
           d[v][i] = dp * w[i];
@@ -273,55 +357,91 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_residual_norm_grad(NormGr
         }
       }
       team_sum<T>(s, lds, turn);
-      along = s[0] * inv;
-      centre = a.post.kind == 2 ? s[1] * inv : 0.0f;
-    } else {
+      const float along = s[0] * inv, centre = post_centred ? s[1] * inv : 0.0f;
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
+        for (int i = 0; i < 8; ++i) d[v][i] = brstd * fmaf(-along, b[v][i], d[v][i] - centre);
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float g[8];
+        if constexpr (kKeep) recall(3, g);
+        else scaled_gate(v, g);
+#pragma unroll
         for (int i = 0; i < 8; ++i) {
-          gs[v][i] = fmaf(a.scale * d[v][i], b[v][i], gs[v][i]);
-          d[v][i] = a.scale * g[v][i] * d[v][i];
+          gs[v][i] = fmaf(d[v][i], b[v][i], gs[v][i]);
+          d[v][i] *= g[i];
         }
+      }
     }
     if (a.db) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (post) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) d[v][i] = rstd * (d[v][i] - centre - b[v][i] * along);
-        }
-        if (in[v]) store8<DT>(a.db, row * a.lddb + col[v], left[v], d[v]);
-      }
+      for (int v = 0; v < V; ++v) store8<DT>(a.db, row * a.lddb + col[v], left[v], d[v]);
     }
   }
-  if (a.rows_per_gate && a.dgate && r0 < r1) flush_gate(group);
+  if (a.rows_per_gate && a.dgate) flush_gate();
   if (!a.sums) return;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if (!in[v]) continue;
     const int64_t at = team * kNormVectors * a.cols + col[v];
     if (a.dnw) store8<kFP32>(a.sums, at, left[v], nw[v]);
     if (a.dnb) store8<kFP32>(a.sums, at + a.cols, left[v], nb[v]);
     if (a.dpw) store8<kFP32>(a.sums, at + 2 * a.cols, left[v], pw[v]);
     if (a.dpb) store8<kFP32>(a.sums, at + 3 * a.cols, left[v], pb[v]);
-    if (a.dgate && !a.rows_per_gate) store8<kFP32>(a.sums, at + 4 * a.cols, left[v], gs[v]);
+    if (a.dgate && !a.rows_per_gate) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) gs[v][i] *= a.scale;
+      store8<kFP32>(a.sums, at + 4 * a.cols, left[v], gs[v]);
+    }
   }
 }
 
-// The gates' gradients of groups of rows that more than one team had a part of, teams in order.
-__global__ __launch_bounds__(256) void k_gate_groups(NormGradArgs a) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.cols) return;
-  const int64_t groups = (a.rows + a.rows_per_gate - 1) / a.rows_per_gate;
-  for (int64_t g = blockIdx.y; g < groups; g += gridDim.y) {
-    const int64_t g0 = g * a.rows_per_gate, g1 = g0 + a.rows_per_gate < a.rows ? g0 + a.rows_per_gate : a.rows;
-    const int64_t t0 = g0 / a.rows_per_team, t1 = (g1 - 1) / a.rows_per_team;
-    if (t0 == t1) continue;  // written by its team
+// The teams' sums added up, in an order that depends on their number alone: 64 columns of a vector per workgroup, the teams
+// dealt to its 16 wavefronts.  Vectors 0 .. 4, and behind them the gates of groups of rows that more than one team had a part of.
+__global__ __launch_bounds__(1024) void k_norm_vectors(NormGradArgs a, int64_t entries) {
+  __shared__ float all[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+  void* const outs[kNormVectors] = {a.dnw, a.dnb, a.dpw, a.dpb, a.rows_per_gate ? nullptr : a.dgate};
+  for (int64_t e = blockIdx.y; e < entries; e += gridDim.y) {
+    void* out = nullptr;
+    const float* p = nullptr;
+    int64_t stride = 0, at = 0, first = 0;  // term t is p[t * stride], the first one p[first]
+    int count = 0;
+    if (e < kNormVectors) {
+      out = e == 0 ? outs[0] : e == 1 ? outs[1] : e == 2 ? outs[2] : e == 3 ? outs[3] : outs[4];
+      p = a.sums + e * a.cols;
+      stride = kNormVectors * a.cols;
+      count = a.teams;
+    } else {
+      const int64_t g = e - kNormVectors;
+      const int64_t g0 = g * a.rows_per_gate, g1 = g0 + a.rows_per_gate < a.rows ? g0 + a.rows_per_gate : a.rows;
+      const int64_t t0 = g0 / a.rows_per_team, t1 = (g1 - 1) / a.rows_per_team;
+      if (t0 == t1) continue;  // its team has written it
+      out = a.dgate;
+      at = g * a.cols;
+      p = a.gate_edges + t0 * 2 * a.cols;
+      stride = 2 * a.cols;
+      first = t0 * a.rows_per_team / a.rows_per_gate == g ? 0 : a.cols;  // the others begin in this group
+      count = (int)(t1 - t0 + 1);
+    }
+    if (!out) continue;
     float s = 0.0f;
-    for (int64_t t = t0; t <= t1; ++t)
-      s += as_global<float>(a.gate_edges)[(t * 2 + (t * a.rows_per_team / a.rows_per_gate == g ? 0 : 1)) * a.cols + c];
-    store1_of(a.vec_dtype, a.dgate, g * a.cols + c, s);
+    if (c < a.cols) {
+      const auto q = as_global<float>(p) + c;
+#pragma unroll 4
+      for (int t = wave; t < count; t += 16) s += q[t == 0 ? first : t * stride];
+    }
+    all[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < a.cols) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) sum += all[w][lane];
+      store1_of(a.vec_dtype, out, at + c, sum);
+    }
+    __syncthreads();
   }
 }
 
@@ -336,15 +456,19 @@ hipError_t forward(const NormArgs& a, hipStream_t stream) {
   else k_residual_norm<DT, 1024, 2><<<rows, 1024, 0, stream>>>(a);
   return hipGetLastError();
 }
+template <int DT, int T, int V>
+void backward_of(const NormGradArgs& a, hipStream_t stream) {
+  if (a.cols == T * V * 8) k_residual_norm_grad<DT, T, V, true><<<dim3((uint32_t)a.teams), T, 0, stream>>>(a);
+  else k_residual_norm_grad<DT, T, V, false><<<dim3((uint32_t)a.teams), T, 0, stream>>>(a);
+}
 template <int DT>
 hipError_t backward(const NormGradArgs& a, hipStream_t stream) {
-  const uint32_t teams = (uint32_t)a.teams, quarter = (uint32_t)ceil_div(a.teams, 4);
-  if (a.cols <= 512) k_residual_norm_grad<DT, 64, 1><<<quarter, 256, 0, stream>>>(a);
-  else if (a.cols <= 1024) k_residual_norm_grad<DT, 64, 2><<<quarter, 256, 0, stream>>>(a);
-  else if (a.cols <= 2048) k_residual_norm_grad<DT, 256, 1><<<teams, 256, 0, stream>>>(a);
-  else if (a.cols <= 4096) k_residual_norm_grad<DT, 256, 2><<<teams, 256, 0, stream>>>(a);
-  else if (a.cols <= 8192) k_residual_norm_grad<DT, 512, 2><<<teams, 512, 0, stream>>>(a);
-  else k_residual_norm_grad<DT, 1024, 2><<<teams, 1024, 0, stream>>>(a);
+  if (a.cols <= 512) backward_of<DT, 64, 1>(a, stream);
+  else if (a.cols <= 1024) backward_of<DT, 128, 1>(a, stream);
+  else if (a.cols <= 2048) backward_of<DT, 256, 1>(a, stream);
+  else if (a.cols <= 4096) backward_of<DT, 512, 1>(a, stream);
+  else if (a.cols <= 8192) backward_of<DT, 1024, 1>(a, stream);
+  else backward_of<DT, 1024, 2>(a, stream);
   return hipGetLastError();
 }
 
@@ -355,7 +479,8 @@ hipError_t launch_residual_norm(int dtype, const NormArgs& a, hipStream_t stream
 }
 
 void norm_grad_teams(int64_t rows, int64_t cols, int32_t& teams, int64_t& rows_per_team) {
-  const int64_t most = cols <= 1024 ? 2048 : 512;
+  // workgroups that the 256 CUs hold at a time: 16 wavefronts on each
+  const int64_t most = cols <= 512 ? 4096 : cols <= 1024 ? 2048 : cols <= 2048 ? 1024 : cols <= 4096 ? 512 : 256;
   rows_per_team = ceil_div(rows, most);
   if (rows_per_team < 1) rows_per_team = 1;
   teams = (int32_t)ceil_div(rows, rows_per_team);
@@ -364,15 +489,9 @@ void norm_grad_teams(int64_t rows, int64_t cols, int32_t& teams, int64_t& rows_p
 hipError_t launch_residual_norm_grad(int dtype, const NormGradArgs& a, hipStream_t stream) {
   const hipError_t e = dtype == kFP16 ? backward<kFP16>(a, stream) : dtype == kBF16 ? backward<kBF16>(a, stream) : backward<kFP32>(a, stream);
   if (e != hipSuccess) return e;
-  const bool grouped = a.dgate && a.rows_per_gate;
-  if (grouped) {
-    const int64_t groups = ceil_div(a.rows, a.rows_per_gate);
-    k_gate_groups<<<dim3((uint32_t)ceil_div(a.cols, 256), (uint32_t)(groups < 4096 ? groups : 4096)), 256, 0, stream>>>(a);
-  }
-  if (a.dnw || a.dnb || a.dpw || a.dpb || (a.dgate && !grouped)) {
-    ColumnSums s{a.sums, a.cols, kNormVectors * a.cols, a.teams, kNormVectors, a.vec_dtype, {a.dnw, a.dnb, a.dpw, a.dpb, grouped ? nullptr : a.dgate}};
-    return launch_column_sums(s, stream);
-  }
+  const int64_t groups = a.dgate && a.rows_per_gate ? ceil_div(a.rows, a.rows_per_gate) : 0, entries = kNormVectors + groups;
+  if (!a.sums && !groups) return hipSuccess;
+  k_norm_vectors<<<dim3((uint32_t)ceil_div(a.cols, 64), (uint32_t)(entries < 1024 ? entries : 1024)), 1024, 0, stream>>>(a, entries);
   return hipGetLastError();
 }
 

@@ -77,8 +77,8 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a, Drop drop) {
   }
 }
 
-// 64 columns of one vector per workgroup, the blocks dealt to four wavefronts.
-__global__ __launch_bounds__(256) void k_column_sums(ColumnSums a) {
+// 64 columns of one vector per workgroup, the blocks dealt to its 16 wavefronts.
+__global__ __launch_bounds__(1024) void k_column_sums(ColumnSums a) {
   const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
   const int64_t c = (int64_t)blockIdx.x * 64 + lane;
   void* out = a.out[blockIdx.y];
@@ -86,12 +86,18 @@ __global__ __launch_bounds__(256) void k_column_sums(ColumnSums a) {
   float s = 0.0f;
   if (c < a.cols) {
     const auto p = as_global<float>(a.sums) + (int64_t)blockIdx.y * a.cols + c;
-    for (int b = part; b < a.blocks; b += 4) s += p[(int64_t)b * a.stride];
+#pragma unroll 4
+    for (int b = part; b < a.blocks; b += 16) s += p[(int64_t)b * a.stride];
   }
-  __shared__ float all[4][64];
+  __shared__ float all[16][64];
   all[part][lane] = s;
   __syncthreads();
-  if (part == 0 && c < a.cols) store1_of(a.dtype, out, c, (all[0][lane] + all[1][lane]) + (all[2][lane] + all[3][lane]));
+  if (part == 0 && c < a.cols) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) sum += all[w][lane];
+    store1_of(a.dtype, out, c, sum);
+  }
 }
 
 // Eight elements per lane; a wavefront has 512 neighbouring columns of one row.
@@ -130,7 +136,7 @@ hipError_t launch_slope(int dtype, bool gated, const SlopeArgs& a, hipStream_t s
 }
 
 hipError_t launch_column_sums(const ColumnSums& a, hipStream_t stream) {
-  k_column_sums<<<dim3((uint32_t)ceil_div(a.cols, 64), (uint32_t)a.vectors), 256, 0, stream>>>(a);
+  k_column_sums<<<dim3((uint32_t)ceil_div(a.cols, 64), (uint32_t)a.vectors), 1024, 0, stream>>>(a);
   return hipGetLastError();
 }
 

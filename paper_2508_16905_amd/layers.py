@@ -26,6 +26,7 @@ from . import binding as B
 _CODE = {torch.float16: B.FP16, torch.bfloat16: B.BF16, torch.float32: B.FP32}
 _ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 _KIND = {"rms": 1, "layer": 2}
+_SIZE = {args: C.sizeof(args) for args, _ in B._LAYER_CALLS.values()}
 
 
 class Dropout(NamedTuple):
@@ -63,42 +64,53 @@ def _refuse(name: str, why: str):
 
 
 def _matrix(t: torch.Tensor, name: str, cols: int = 0, like: Optional[torch.Tensor] = None, rows: int = -1):
-    """(address, row stride, rows, columns) of a matrix."""
+    """(address, row stride, rows, columns) of a matrix.  (A call on few rows is bound by what happens here: the usual tensor
+    of two dimensions goes the shortest way.)"""
     if not t.is_cuda:
         _refuse(name, "a tensor on the GPU is wanted")
-    if t.dtype not in _CODE:
-        _refuse(name, f"float16, bfloat16 or float32 is wanted, not {t.dtype}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+    if like is None:
+        if t.dtype not in _CODE:
+            _refuse(name, f"float16, bfloat16 or float32 is wanted, not {t.dtype}")
+    elif t.dtype is not like.dtype or t.get_device() != like.get_device():
         _refuse(name, f"type or device differs from the call's ({like.dtype}, {like.device})")
-    dim = t.dim()
-    if dim == 0 or t.shape[-1] == 0:
+    if t.dim() == 2:
+        m, n = t.shape
+        ld, one = t.stride()
+        if m == 1:
+            ld = n
+    else:
+        m, ld, n, one = _rows_of(t, name)
+    if n == 0:
         _refuse(name, "at least one column is wanted")
-    n = t.shape[-1]
     if cols and n != cols:
         _refuse(name, f"{n} columns where the call has {cols}")
-    if dim == 2:
-        m, ld = t.shape[0], t.stride(0)
-    elif dim == 1:
-        m, ld = 1, n
-    else:
-        m, ld, step = t.numel() // n, 0, 0
-        if m:
-            for i in range(dim - 2, -1, -1):   # the leading dimensions have to be one run of rows
-                if t.shape[i] > 1:
-                    if ld == 0:
-                        ld = step = t.stride(i)
-                    elif t.stride(i) != step:
-                        _refuse(name, "the leading dimensions do not lie one after another: make it contiguous")
-                    step *= t.shape[i]
     if rows >= 0 and m != rows:
         _refuse(name, f"{m} rows where the call has {rows}")
-    if n > 1 and t.stride(-1) != 1:
+    if one != 1 and n > 1:
         _refuse(name, "the last dimension has to have stride 1")
-    if m <= 1:
+    if m == 0:
         ld = n
-    if ld < n:
+    elif ld < n:
         _refuse(name, "rows overlap (an expanded tensor): make it contiguous")
     return t.data_ptr(), ld, m, n
+
+
+def _rows_of(t: torch.Tensor, name: str):
+    """(rows, row stride, columns, column stride) of any number of dimensions but two."""
+    if t.dim() == 0:
+        _refuse(name, "at least one dimension is wanted")
+    n = t.shape[-1]
+    m = t.numel() // n if n else 0
+    ld = step = 0
+    if m:
+        for i in range(t.dim() - 2, -1, -1):   # the leading dimensions have to be one run of rows
+            if t.shape[i] > 1:
+                if ld == 0:
+                    ld = step = t.stride(i)
+                elif t.stride(i) != step:
+                    _refuse(name, "the leading dimensions do not lie one after another: make it contiguous")
+                step *= t.shape[i]
+    return m, n if m <= 1 else ld, n, t.stride(-1)
 
 
 def _vector(t: Optional[torch.Tensor], name: str, n: int, like: torch.Tensor):
@@ -112,9 +124,12 @@ def _vector(t: Optional[torch.Tensor], name: str, n: int, like: torch.Tensor):
     return t.data_ptr(), _CODE[t.dtype]
 
 
+_NO_DROP = B.DropoutSpec(0.0, 0, 0, None)
+
+
 def _drop(d: Optional[Dropout], like: torch.Tensor):
     if d is None:
-        return B.DropoutSpec(0.0, 0, 0, None)
+        return _NO_DROP
     if d.state is None:
         return B.DropoutSpec(d.p, d.seed & 0xFFFFFFFFFFFFFFFF, d.offset & 0xFFFFFFFFFFFFFFFF, None)
     if d.state.dtype != torch.int64 or d.state.numel() != 2 or not d.state.is_contiguous() or d.state.device != like.device:
@@ -128,45 +143,39 @@ def _act(name: str) -> int:
     return _ACT[name]
 
 
+_calls = {}
+
+
+def _functions(name: str):
+    """(the call, its workspace query or None) in the library."""
+    lib = B.load_library()
+    found = getattr(lib, name), getattr(lib, name + "_workspace") if B._LAYER_CALLS[name][1] else None
+    _calls[name] = found
+    return found
+
+
 def _call(name: str, args, like: torch.Tensor):
-    lib = B._lib or B.load_library()
-    workspace = getattr(lib, name + "_workspace", None) if B._LAYER_CALLS[name][1] else None
-    with _On(like.device):
-        keep = None
-        if workspace is not None:
-            size = workspace(C.byref(args))
-            if size < 0:
-                raise B.TriAccelError(int(size), name)
-            if size:
-                keep = torch.empty(size, dtype=torch.uint8, device=like.device)
-                args.workspace, args.workspace_bytes = keep.data_ptr(), size
-        code = getattr(lib, name)(C.byref(args), torch.cuda.current_stream(like.device).cuda_stream)
+    device = like.get_device()
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _call(name, args, like)
+    call, workspace = _calls.get(name) or _functions(name)
+    at, keep = C.byref(args), None
+    if workspace is not None:
+        size = workspace(at)
+        if size < 0:
+            raise B.TriAccelError(int(size), name)
+        if size:
+            keep = torch.empty(size, dtype=torch.uint8, device=like.device)
+            args.workspace, args.workspace_bytes = keep.data_ptr(), size
+    code = call(at, torch._C._cuda_getCurrentRawStream(device))  # current_stream() makes an object first: 2 us
     if code != 0:
         raise B.TriAccelError(code, name)
 
 
-class _On:
-    """The tensors' device as the current one, where it is not already."""
-
-    __slots__ = ("at", "before")
-
-    def __init__(self, device):
-        self.at, self.before = device.index, None
-
-    def __enter__(self):
-        now = torch.cuda.current_device()
-        if now != self.at:
-            self.before = now
-            torch.cuda.set_device(self.at)
-
-    def __exit__(self, *_):
-        if self.before is not None:
-            torch.cuda.set_device(self.before)
-
-
 def _new(like: torch.Tensor, cols: int) -> torch.Tensor:
     """A dense matrix of the leading dimensions of ``like``."""
-    return torch.empty(*like.shape[:-1], cols, dtype=like.dtype, device=like.device)
+    return like.new_empty((*like.shape[:-1], cols))
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
@@ -181,7 +190,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     y = _new(x, n) if out is None else out
     py, ldy = _matrix(y, "out", n, x, rows)[:2]
     pre = _new(x, n) if save else None
-    args = B.LinearArgs(C.sizeof(B.LinearArgs), _CODE[x.dtype], rows, k, n, px, ldx, pw, ldw, pb, pr, ldr, py, ldy,
+    args = B.LinearArgs(_SIZE[B.LinearArgs], _CODE[x.dtype], rows, k, n, px, ldx, pw, ldw, pb, pr, ldr, py, ldy,
                         pre.data_ptr() if save else None, n, bias_code, _act(act), scale, 0, _drop(dropout, x), None, 0)
     _call("triaccel_linear", args, x)
     return (y, pre) if save else y
@@ -204,7 +213,7 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre
     db = torch.empty(n, dtype=torch.float32, device=dy.device) if bias_grad else None
     if dw is not None and dw.dtype not in (dy.dtype, torch.float32):
         _refuse("weight_grad_dtype", "the type of the call or float32 is wanted")
-    args = B.LinearBackwardArgs(C.sizeof(B.LinearBackwardArgs), _CODE[dy.dtype], rows, k, n, pd, lddy, px, ldx, pw, ldw, pp, ldp,
+    args = B.LinearBackwardArgs(_SIZE[B.LinearBackwardArgs], _CODE[dy.dtype], rows, k, n, pd, lddy, px, ldx, pw, ldw, pp, ldp,
                                 dx.data_ptr() if x_grad else None, k, dw.data_ptr() if weight_grad else None, k,
                                 db.data_ptr() if bias_grad else None, _CODE[dw.dtype] if weight_grad else B.FP32, B.FP32, code, scale,
                                 _drop(dropout, dy), None, 0)
@@ -227,7 +236,7 @@ def gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, b_gate: Opt
         _refuse("b_up", "both biases, of one type, or none")
     h = _new(x, n)
     g, u = (_new(x, n), _new(x, n)) if save else (None, None)
-    args = B.GatedArgs(C.sizeof(B.GatedArgs), _CODE[x.dtype], rows, k, n, px, ldx, pg, pu, ldw, bg, bu, h.data_ptr(), n,
+    args = B.GatedArgs(_SIZE[B.GatedArgs], _CODE[x.dtype], rows, k, n, px, ldx, pg, pu, ldw, bg, bu, h.data_ptr(), n,
                        g.data_ptr() if save else None, u.data_ptr() if save else None, n, bias_code, _act(act), None, 0)
     _call("triaccel_gated", args, x)
     return (h, g, u) if save else h
@@ -253,7 +262,7 @@ def gated_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up
     dx = _new(x, k) if x_grad else None
     dwg, dwu = (torch.empty(n, k, dtype=dt, device=dh.device), torch.empty(n, k, dtype=dt, device=dh.device)) if weight_grad else (None, None)
     dbg, dbu = (torch.empty(n, device=dh.device), torch.empty(n, device=dh.device)) if bias_grad else (None, None)
-    args = B.GatedBackwardArgs(C.sizeof(B.GatedBackwardArgs), _CODE[dh.dtype], rows, k, n, pd, lddh, px, ldx, pg, pu, ldw, qg, qu, ldg,
+    args = B.GatedBackwardArgs(_SIZE[B.GatedBackwardArgs], _CODE[dh.dtype], rows, k, n, pd, lddh, px, ldx, pg, pu, ldw, qg, qu, ldg,
                                dx.data_ptr() if x_grad else None, k, dwg.data_ptr() if weight_grad else None,
                                dwu.data_ptr() if weight_grad else None, k, dbg.data_ptr() if bias_grad else None,
                                dbu.data_ptr() if bias_grad else None, _CODE[dt], B.FP32, _act(act), 0, None, 0)
@@ -297,7 +306,7 @@ def residual_norm(residual: torch.Tensor, block: Optional[torch.Tensor] = None, 
     pg, ldg, gate_code = _gate(gate, rows_per_gate, rows, n, residual)
     out = _new(residual, n) if block is not None else residual
     y = _new(residual, n) if norm is not None else None
-    args = B.ResidualNormArgs(C.sizeof(B.ResidualNormArgs), _CODE[residual.dtype], rows, n, pr, ldr, pb, ldb, pg, ldg, rows_per_gate,
+    args = B.ResidualNormArgs(_SIZE[B.ResidualNormArgs], _CODE[residual.dtype], rows, n, pr, ldr, pb, ldb, pg, ldg, rows_per_gate,
                               out.data_ptr() if block is not None else None, n, y.data_ptr() if norm is not None else None, n, gate_code, scale,
                               _norm_spec(post, "post", n, residual), _norm_spec(norm, "norm", n, residual))
     _call("triaccel_residual_norm", args, residual)
@@ -330,7 +339,7 @@ def residual_norm_backward(dresidual: Optional[torch.Tensor], dy: Optional[torch
     dpw, dpb = (vector(post.weight), vector(post.bias)) if post is not None else (None, None)
     dnw, dnb = (vector(norm.weight), vector(norm.bias)) if norm is not None else (None, None)
     dr, db = _new(like, n), _new(like, n) if block is not None else None
-    args = B.ResidualNormBackwardArgs(C.sizeof(B.ResidualNormBackwardArgs), _CODE[like.dtype], rows, n, pd, ldd, py, ldy, pr, ldr, pb, ldb,
+    args = B.ResidualNormBackwardArgs(_SIZE[B.ResidualNormBackwardArgs], _CODE[like.dtype], rows, n, pd, ldd, py, ldy, pr, ldr, pb, ldb,
                                       pg, ldg, rows_per_gate, dr.data_ptr(), n, at(db), n, at(dgate), at(dpw), at(dpb), at(dnw), at(dnb),
                                       gate_code, B.FP32, scale, 0, post_spec, norm_spec, None, 0)
     _call("triaccel_residual_norm_backward", args, like)
@@ -344,7 +353,7 @@ def dropout(x: torch.Tensor, drop: Dropout, residual: Optional[torch.Tensor] = N
     pr, ldr = _matrix(residual, "residual", n, x, rows)[:2] if residual is not None else (None, n)
     y = _new(x, n) if out is None else out
     py, ldy = _matrix(y, "out", n, x, rows)[:2]
-    args = B.DropoutArgs(C.sizeof(B.DropoutArgs), _CODE[x.dtype], rows, n, px, ldx, pr, ldr, py, ldy, scale, 0, _drop(drop, x))
+    args = B.DropoutArgs(_SIZE[B.DropoutArgs], _CODE[x.dtype], rows, n, px, ldx, pr, ldr, py, ldy, scale, 0, _drop(drop, x))
     _call("triaccel_dropout", args, x)
     return y
 
