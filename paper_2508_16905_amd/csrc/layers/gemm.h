@@ -10,7 +10,14 @@
 // the parts are kept scaled up, so that those of subnormal numbers do not fall below bf16's own), and of the nine partial
 // products the six largest are summed, those of one scale in one accumulator; what is dropped is at most 2^-26 of a product.
 // Six bf16 products have 2.6 times the rate of the fp32 matrix instructions (2.5 PFLOP/s / 6 = 417 and 157 TFLOP/s).
+//
+// Two forms.  DIRECT: operands of whole, aligned 16-byte units (fp32: their parts, laid out by k_pack) go from memory to LDS
+// without registers, a tile ahead, while the fragments of the next 32 k are read from LDS beside the products of these.
+// Staged: any strides, alignment and sizes through registers, with fp32 split on the way; for small products, where what counts
+// is the number of launches, and where KG groups of wavefronts share the k of one tile.
 #pragma once
+#include <type_traits>
+
 #include "layer_util.h"
 
 namespace triaccel {
@@ -25,8 +32,11 @@ struct GemmArgs {
   int32_t m, n;             // rows and columns of the result (kEpiGated: n columns from each of b and b2)
   int32_t seg, nseg;        // k = nseg segments of `seg`
   int32_t seg_step;         // where segment 1 of A (KC) begins
-  int32_t tiles_m, tiles_n, splits, tiles_per_split;
-  float* partial;           // splits > 1: [splits][m][n or 2 n] sums
+  int64_t a_plane, b_plane; // fp32, DIRECT: elements between the parts
+  int32_t tiles_m, tiles_n;
+  int32_t whole;            // the first `whole` tiles of the result have a workgroup each, the others `splits`, of
+  int32_t splits, per_split;  // `per_split` tiles of k
+  float* partial;           // splits > 1: a tile of sums for each such workgroup
   // epilogue
   void *c, *c2;             // kEpiStore: rows >= csplit of the result are rows of c2, rows crows .. csplit - 1 go nowhere
   int64_t ldc;
@@ -61,9 +71,18 @@ __device__ __forceinline__ void epi_columns(const GemmArgs& g, int64_t col, Colu
     if (g.drop.limit) s.key = drop_key(g.drop);
   }
 }
+// v[n], v[n + 1], ... to the front
+__device__ __forceinline__ void drop_first(float (&v)[8], int n) {
+#pragma unroll
+  for (int bit = 4; bit > 0; bit >>= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i + bit < 8) v[i] = n & bit ? v[i + bit] : v[i];
+}
+// `count` of eight columns from `col` on (fewer where the row ends).
 template <int DT, int EPI>
-__device__ __forceinline__ void epi_row(const GemmArgs& g, const ColumnState& s, int64_t row, int64_t col, float (&v)[8], float (&u)[8]) {
-  const int64_t left = g.n - col;
+__device__ __forceinline__ void epi_row(const GemmArgs& g, const ColumnState& s, int64_t row, int64_t col, int count, float (&v)[8], float (&u)[8]) {
+  const int64_t left = g.n - col < count ? g.n - col : count;
   constexpr bool kExact = DT == kFP32;
   if constexpr (EPI == kEpiStore) {
     const bool second = row >= g.csplit;
@@ -143,44 +162,54 @@ __device__ __forceinline__ f32x4 mfma(s16x8 a, s16x8 b, f32x4 c) {
   else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Rounded to bf16; cut off instead where rounding would make an infinity of a number.
-__device__ __forceinline__ uint32_t part_bits(float x) {
-  const uint32_t b = f32_to_bf16_bits(x);
-  return (b & 0x7fffu) == 0x7f80u ? f2u(x) >> 16 : b;
+// The tile of the result with number `t`: bands of four tile rows, column after column, so that workgroups that run at one
+// time share what they read in L2.
+__device__ __forceinline__ void tile_of(const GemmArgs& g, int t, int& tm, int& tn) {
+  constexpr int kBand = 4;
+  const int band = t / (kBand * g.tiles_n), in = t - band * kBand * g.tiles_n;
+  const int high = g.tiles_m - band * kBand < kBand ? g.tiles_m - band * kBand : kBand;
+  tm = band * kBand + in % high;
+  tn = in / high;
 }
-// fp32 -> three bf16 parts.  A rest is below 2^120 and its multiple below 2^128; what is not finite has no rest.
-__device__ __forceinline__ void split3(const Elem8<kFP32>& v, s16x8 (&out)[3]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t h = part_bits(v[i]);
-    const float r = __builtin_isfinite(v[i]) ? (v[i] - bf16_bits_to_f32(h)) * 256.0f : 0.0f;
-    const uint32_t m = part_bits(r);
-    out[0][i] = (short)h;
-    out[1][i] = (short)m;
-    out[2][i] = (short)part_bits((r - bf16_bits_to_f32(m)) * 256.0f);
-  }
+// Workgroups go to the eight XCDs in turn: each XCD gets a run of neighbouring numbers below `total`.
+__device__ __forceinline__ int on_xcd(int id, int total) {
+  const int xcd = id & 7, per = total >> 3, more = total & 7;
+  return xcd * per + (xcd < more ? xcd : more) + (id >> 3);
 }
 
-template <int DT, int LA, int LB, int BM, int BN, int WR, int WC, int EPI, bool DIRECT>
+template <int DT_, int LA, int LB, int BM_, int BN_, int WR, int WC, int KG, int EPI_, bool DIRECT>
 struct Gemm {
+  static constexpr bool kAByK = LA == KS, kBByK = LB == KS;
+  static constexpr int DT = DT_, BM = BM_, BN = BN_, EPI = EPI_;
   static constexpr int kPlanes = DT == kFP32 ? 3 : 1;
   static constexpr int BK = DT == kFP32 ? 32 : 64;
-  static constexpr int NT = WR * WC * 64;
+  static constexpr int NT = WR * WC * 64;                 // threads of a group
+  static constexpr int kThreads = NT * KG;
   static constexpr int FM = BM / WR / 16, FN = BN / WC / 16;
   static constexpr int kAUnits = BM * BK / 8, kBUnits = BN * BK / 8;
   static constexpr int TA = kAUnits / NT, TB = kBUnits / NT;
   static constexpr int kTile = kPlanes * (BM + BN) * BK;  // elements of one buffer
   static constexpr int kSlabCols = FN * 16, kSlabLd = kSlabCols + 4;
-  static constexpr int kRound = FM < 4 ? FM : 4;          // fragments of rows that its slab holds at a time
+  static constexpr int kRound = FM < 4 ? FM : 4;          // fragments of rows that a wavefront's slab holds at a time
   static constexpr int kSlab = 16 * kRound * kSlabLd;     // floats of a wavefront
-  static constexpr int kTileBytes = 2 * kTile * 2, kSlabBytes = WR * WC * kSlab * 4;
-  static constexpr int kLdsBytes = kTileBytes > kSlabBytes ? kTileBytes : kSlabBytes;
+  static constexpr int kTileBytes = KG * 2 * kTile * 2, kSlabBytes = WR * WC * kSlab * 4, kJoinBytes = (KG - 1) * BM * BN * 4;
+  static constexpr int kMost = kSlabBytes > kJoinBytes ? kSlabBytes : kJoinBytes;
+  static constexpr int kLdsBytes = kTileBytes > kMost ? kTileBytes : kMost;
   // columns of the result that a tile has
   static constexpr int kCols = EPI == kEpiGated ? BN / 2 : BN;
   static_assert(TA >= 1 && TB >= 1 && kAUnits % NT == 0 && kBUnits % NT == 0, "whole units per thread");
   static_assert(EPI != kEpiGated || FN % 2 == 0, "half of a wavefront's columns from each matrix");
-  typedef Elem<DT> E;
+  static_assert(!DIRECT || KG == 1, "groups are for the staged form");
+  typedef typename std::conditional<DIRECT, __bf16, Elem<DT>>::type E;  // DIRECT: any 16 bits
   typedef f32x4 Acc[kPlanes][FM][FN];  // [q]: what counts 2^-8q
+
+  // Where the tile of the result begins whose first row is `r0`, and likewise for columns.  DIRECT: the last tile begins
+  // earlier, so that it lies inside (the plan has m >= BM and n >= kCols); what the one before it has is not stored twice.
+  static __device__ __forceinline__ int origin(int r0, int rows, int size, bool whole_units) {
+    if (!DIRECT) return r0;
+    const int last = (whole_units ? (rows + 7) & ~7 : rows) - size;
+    return r0 < last ? r0 : last;
+  }
 
   // Row of B (0 .. BN - 1) -> its matrix and row there.  With two matrices each wavefront has as many rows of the one as of
   // the other, for the same columns of the result, so that the epilogue has both in one lane.
@@ -200,63 +229,96 @@ struct Gemm {
     int seg, k0, left;  // `left`: k in its segment from k0 on
   };
   static __device__ __forceinline__ At at(const GemmArgs& g, int kt) {
-    const int per = g.seg > 0 ? (g.seg + BK - 1) / BK : 1;
+    const int per = (g.seg + BK - 1) / BK;
     const int s = kt >= per ? 1 : 0;
     const int k0 = (kt - s * per) * BK;
     return At{s, k0, g.seg - k0};
   }
 
-  // --- straight to LDS: aligned operands (see direct_ok) ---
+  // --- straight to LDS ---
+  // The tile lies inside the operand (see origin), so that unit t NT + tid is at a distance from unit tid that all lanes have in
+  // common: one offset per lane, the rest in scalar registers.
+  template <int L, int R, bool IS_B>
+  static __device__ __forceinline__ uint32_t lane_offset(const GemmArgs& g, int tid) {
+    const int ld = (int)(IS_B ? g.ldb : g.lda);
+    if constexpr (L == KC) {
+      const int row = tid / (BK / 8), unit = tile_unit<KC, R, BK>(row, tid % (BK / 8)) % (BK / 8);
+      bool second;
+      return (uint32_t)((IS_B ? b_row(row, second) : row) * ld + unit * 8) * 2u;
+    } else {
+      const int k = tid / (R / 8), unit = tile_unit<KS, R, BK>(k, tid % (R / 8)) % (R / 8);
+      return (uint32_t)(k * ld + unit * 8) * 2u;
+    }
+  }
   template <int L, int R, int T, bool IS_B>
-  static __device__ __forceinline__ void issue(const GemmArgs& g, const At& w, int r0, int rows, short* tile, int tid) {
-    const int64_t ld = IS_B ? g.ldb : g.lda;
-    const bool full = w.left >= BK;
-    const E* p0 = (const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a);
-    const E* p1 = (const E*)g.b2;
+  static __device__ __forceinline__ void issue(const GemmArgs& g, const At& w, int r0, uint32_t off, short* tile, int tid) {
+    const int64_t ld = IS_B ? g.ldb : g.lda, plane = IS_B ? g.b_plane : g.a_plane;
     const int64_t koff = (IS_B ? 0 : (int64_t)w.seg * g.seg_step) + w.k0;
     const int64_t skip = L == KC ? (int64_t)r0 * ld + koff : koff * ld + r0;
+    const char* p0 = (const char*)((const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a) + skip);
+    const char* p1 = (const char*)((const E*)g.b2 + skip);
+    constexpr int kStep = L == KC ? NT / (BK / 8) : NT / (R / 8);  // rows, or k, from one t to the next
+    static_assert(kStep % 16 == 0 || (L == KC && kStep % 8 == 0), "the exchange of units is the same for all t");
+    const bool full = w.left >= BK;
+    uint32_t id = (uint32_t)tid;
+    if (!full) asm volatile("" : "+v"(id));  // what follows from it is not worth registers throughout the loop
+    // 0 inside the operand's k, else where the unit's zeros are
+    const auto outside = [&](int t) {
+      if constexpr (L == KC) return (int)(tile_unit<KC, R, BK>((int)id / (BK / 8), (int)id % (BK / 8)) % (BK / 8)) * 8 >= w.left;
+      else return (int)id / (R / 8) + t * kStep >= w.left;
+    };
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      const int slot = t * NT + tid;
-      const char* src;
-      if constexpr (L == KC) {
-        const int row = slot / (BK / 8), unit = (tile_unit<KC, R, BK>(row, slot % (BK / 8))) % (BK / 8);
-        bool second = false;
-        int r = IS_B ? b_row(row, second) : row;
-        r = r0 + r < rows ? r : rows - 1 - r0;
-        src = (const char*)((second ? p1 : p0) + skip) + (uint32_t)(r * (int)ld + unit * 8) * 2u;
-        if (!full && unit * 8 >= w.left) src = (const char*)kZeroPage;
-      } else {
-        const int k = slot / (R / 8), unit = (tile_unit<KS, R, BK>(k, slot % (R / 8))) % (R / 8);
-        int c = unit * 8;
-        c = r0 + c < rows ? c : ((rows + 7) & ~7) - 8 - r0;  // the row's stride has room for whole units
-        src = (const char*)(p0 + skip) + (uint32_t)(k * (int)ld + c) * 2u;
-        if (!full && k >= w.left) src = (const char*)kZeroPage;
+      const char* base = p0;
+      int64_t step = t * kStep * ld * 2;
+      if constexpr (EPI == kEpiGated && IS_B && L == KC) {
+        // rows t kStep ... of the tile, all in one matrix for a wavefront: kStep and its 8 or 16 rows divide kHalf's
+        bool second;
+        const int wave_row = (int)__builtin_amdgcn_readfirstlane((uint32_t)tid) / (BK / 8);
+        const int row = b_row(t * kStep + wave_row, second);
+        if (second) base = p1;
+        step = (row - wave_row) * ld * 2;
+        // the lane's offset was made from b_row(row of tid), which is wave_row plus the same as here
+        bool ignored;
+        step += (wave_row - b_row(wave_row, ignored)) * ld * 2;
       }
-      // lane i's 16 bytes go to the wavefront's place plus 16 i: slot `slot`
-      __builtin_amdgcn_global_load_lds((const TA_GLOBAL char*)src,
-                                       (__attribute__((address_space(3))) char*)tile + (t * NT + (tid & ~63)) * 16, 16, 0, 0);
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q) {
+        const char* src = base + step + q * plane * 2 + off;
+        if (!full) src = outside(t) ? (const char*)kZeroPage : src;
+        // lane i's 16 bytes go to the wavefront's place plus 16 i
+        __builtin_amdgcn_global_load_lds((const TA_GLOBAL char*)src,
+                                         (__attribute__((address_space(3))) char*)tile + q * R * BK * 2 + (t * NT + (tid & ~63)) * 16, 16, 0, 0);
+      }
     }
   }
 
-  // --- through registers: any alignment, any strides, any sizes ---
+  // --- through registers ---
   template <int L, int R, int T, bool IS_B>
   static __device__ __forceinline__ void fetch(const GemmArgs& g, const At& w, int r0, int rows, Elem8<DT> (&out)[T], int tid) {
     const int64_t ld = IS_B ? g.ldb : g.lda;
-    const E* p = (const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a);
-    const int64_t koff = (IS_B ? 0 : (int64_t)w.seg * g.seg_step) + w.k0;
+    const int64_t seg0 = IS_B ? 0 : (int64_t)w.seg * g.seg_step;
+    const E* p0 = (const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a);
+    const bool inside = w.left >= BK && (L == KC || r0 + R <= rows);
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       const int slot = t * NT + tid;
       if constexpr (L == KC) {
         const int row = slot / (BK / 8), unit = slot % (BK / 8);
         bool second = false;
-        const int r = r0 + (IS_B ? b_row(row, second) : row);
-        const E* q = second ? (const E*)g.b2 : p;
-        out[t] = load_raw8<DT>(q + (int64_t)r * ld + koff + unit * 8, r < rows ? w.left - unit * 8 : 0);
+        int r = r0 + (IS_B ? b_row(row, second) : row);
+        r = r < rows ? r : rows - 1;  // a row of the result that is not written
+        const E* q = (second ? (const E*)g.b2 : p0) + (int64_t)r * ld + seg0;
+        out[t] = inside ? load_raw8<DT>(q + w.k0 + unit * 8) : load_edge8<DT>(q, w.k0 + unit * 8, g.seg);
       } else {
         const int k = slot / (R / 8), c = r0 + slot % (R / 8) * 8;
-        out[t] = load_raw8<DT>(p + (koff + k) * ld + c, k < w.left ? rows - c : 0);
+        const E* q = p0 + (seg0 + w.k0 + (k < w.left ? k : w.left - 1)) * ld;
+        if (inside) {
+          out[t] = load_raw8<DT>(q + c);
+        } else {
+          out[t] = load_edge8<DT>(q, c, rows);
+          if (k >= w.left) out[t] = Elem8<DT>{};
+        }
       }
     }
   }
@@ -277,46 +339,52 @@ struct Gemm {
     }
   }
 
-  static __device__ __forceinline__ void multiply(const short* tile, Acc& acc, int wm, int wn, int lane) {
-    const short* ta = tile;
+  // --- products of 32 k ---
+  struct Frags {
+    s16x8 a[FM][kPlanes], b[FN][kPlanes];
+  };
+  static __device__ __forceinline__ void read(Frags& f, const short* tile, int k0, int wm, int wn, int lane) {
     const short* tb = tile + kPlanes * BM * BK;
 #pragma unroll
-    for (int k0 = 0; k0 < BK; k0 += 32) {
-      s16x8 b[FN][kPlanes];
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
+      for (int q = 0; q < kPlanes; ++q) f.b[j][q] = fragment<LB, BN, BK>(tb + q * BN * BK, wn * FN * 16 + j * 16, k0, lane);
 #pragma unroll
-        for (int q = 0; q < kPlanes; ++q) b[j][q] = fragment<LB, BN, BK>(tb + q * BN * BK, wn * FN * 16 + j * 16, k0, lane);
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        s16x8 a[kPlanes];
+      for (int q = 0; q < kPlanes; ++q) f.a[i][q] = fragment<LA, BM, BK>(tile + q * BM * BK, wm * FM * 16 + i * 16, k0, lane);
+  }
+  static __device__ __forceinline__ void multiply(Acc& acc, const Frags& f) {
+    // B first: a lane then has four neighbouring columns of one row of the result
 #pragma unroll
-        for (int q = 0; q < kPlanes; ++q) a[q] = fragment<LA, BM, BK>(ta + q * BM * BK, wm * FM * 16 + i * 16, k0, lane);
-        // B first: a lane then has four neighbouring columns of one row of the result
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          if constexpr (kPlanes == 3) {
-            acc[2][i][j] = mfma<kBF16>(b[j][2], a[0], acc[2][i][j]);
-            acc[1][i][j] = mfma<kBF16>(b[j][1], a[0], acc[1][i][j]);
-            acc[0][i][j] = mfma<kBF16>(b[j][0], a[0], acc[0][i][j]);
-            acc[2][i][j] = mfma<kBF16>(b[j][0], a[2], acc[2][i][j]);
-            acc[1][i][j] = mfma<kBF16>(b[j][0], a[1], acc[1][i][j]);
-            acc[2][i][j] = mfma<kBF16>(b[j][1], a[1], acc[2][i][j]);
-          } else {
-            acc[0][i][j] = mfma<DT>(b[j][0], a[0], acc[0][i][j]);
-          }
+      for (int j = 0; j < FN; ++j) {
+        const s16x8 *a = f.a[i], *b = f.b[j];
+        if constexpr (kPlanes == 3) {
+          acc[2][i][j] = mfma<kBF16>(b[2], a[0], acc[2][i][j]);
+          acc[1][i][j] = mfma<kBF16>(b[1], a[0], acc[1][i][j]);
+          acc[0][i][j] = mfma<kBF16>(b[0], a[0], acc[0][i][j]);
+          acc[2][i][j] = mfma<kBF16>(b[0], a[2], acc[2][i][j]);
+          acc[1][i][j] = mfma<kBF16>(b[0], a[1], acc[1][i][j]);
+          acc[2][i][j] = mfma<kBF16>(b[1], a[1], acc[2][i][j]);
+        } else {
+          acc[0][i][j] = mfma<DT>(b[0], a[0], acc[0][i][j]);
         }
       }
-    }
   }
 
   // Up to 64 rows at a time through the wavefront's own slab of LDS: a lane's four columns become eight of one row, so that
-  // bias, dropout's generator, residual and stores work on 16 bytes.
-  static __device__ __forceinline__ void finish(const GemmArgs& g, const f32x4 (&acc)[FM][FN], float* slab, int row0, int col0, int lane, int split) {
+  // bias, dropout's generator, residual and stores work on 16 bytes.  `partial`: the sums of a tile whose k is shared go to a
+  // tile of fp32 instead.
+  static __device__ __forceinline__ void finish(const GemmArgs& g, const f32x4 (&acc)[FM][FN], float* slab, int tm, int tn, int r0, int c0, int wm, int wn, int lane, float* partial) {
     constexpr int kOut = EPI == kEpiGated ? kSlabCols / 2 : kSlabCols, kLanes = kOut / 8, kRows = 64 / kLanes < 16 ? 64 / kLanes : 16;
-    const int col = col0 + lane % kLanes * 8, sub = lane / kLanes;
-    const bool mine = col < g.n && sub < kRows;
-    const bool partial = g.splits > 1;
+    const int in_col = wn * kOut + lane % kLanes * 8, in_row = wm * FM * 16;
+    const int row0 = r0 + in_row, sub = lane / kLanes;
+    int col = c0 + in_col;
+    const int over = tn * kCols - col;  // columns of the eight that the tile before has
+    const bool mine = sub < kRows && (partial || (col < g.n && over < 8));
+    if (over > 0) col += over;
     ColumnState state;
     if (!partial) epi_columns<EPI>(g, col, state);
     static_assert(FM % kRound == 0, "whole rounds");
@@ -330,7 +398,7 @@ struct Gemm {
 #pragma unroll 1
       for (int r = sub; r < 16 * kRound; r += kRows) {
         const int row = row0 + h * 16 + r;
-        if (mine && row < g.m) {
+        if (mine && (partial || (row < g.m && row >= tm * BM))) {
           const float* q = slab + r * kSlabLd + lane % kLanes * 8;
           float v[8], u[8];
           *(f32x4*)v = *(const f32x4*)q;
@@ -340,12 +408,17 @@ struct Gemm {
             *(f32x4*)(u + 4) = *(const f32x4*)(q + kOut + 4);
           }
           if (partial) {
-            const int64_t width = EPI == kEpiGated ? 2 * (int64_t)g.n : g.n;
-            const int64_t base = ((int64_t)split * g.m + row) * width + col;
-            store8<kFP32>(g.partial, base, g.n - col, v);
-            if constexpr (EPI == kEpiGated) store8<kFP32>(g.partial, base + g.n, g.n - col, u);
+            const int64_t base = (in_row + h * 16 + r) * BN + in_col;
+            store8<kFP32>(partial, base, 8, v);
+            if constexpr (EPI == kEpiGated) store8<kFP32>(partial, base + kCols, 8, u);
           } else {
-            epi_row<DT, EPI>(g, state, row, col, v, u);
+            int count = 8;
+            if (DIRECT && over > 0) {
+              count -= over;
+              drop_first(v, over);
+              if constexpr (EPI == kEpiGated) drop_first(u, over);
+            }
+            epi_row<DT, EPI>(g, state, row, col, count, v, u);
           }
         }
       }
@@ -353,72 +426,120 @@ struct Gemm {
     }
   }
 
-  // Workgroups go to the eight XCDs in turn.  Each XCD gets a run of neighbouring tiles, four tile rows at a time, so that what
-  // its workgroups read at one time is shared in its L2.
-  static __device__ __forceinline__ void place_of(const GemmArgs& g, int& tm, int& tn, int& split) {
-    const int total = g.tiles_m * g.tiles_n * g.splits, id = blockIdx.x;
-    const int xcd = id & 7, per = total >> 3, more = total & 7;
-    const int lin = xcd * per + (xcd < more ? xcd : more) + (id >> 3);
-    const int tiles = g.tiles_m * g.tiles_n;
-    split = lin / tiles;
-    const int t = lin - split * tiles;
-    constexpr int kGroup = 4;
-    const int band = t / (kGroup * g.tiles_n), in = t - band * kGroup * g.tiles_n;
-    const int high = g.tiles_m - band * kGroup < kGroup ? g.tiles_m - band * kGroup : kGroup;
-    tm = band * kGroup + in % high;
-    tn = in / high;
-  }
-
-  static __device__ __forceinline__ void run(const GemmArgs& g, short* lds) {
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WC, wn = wave % WC;
-    int tm, tn, split;
-    place_of(g, tm, tn, split);
-    const int r0 = tm * BM, c0 = tn * kCols;
-    const int all = g.seg > 0 ? (g.seg + BK - 1) / BK * g.nseg : 0;
-    const int first = split * g.tiles_per_split, last = first + g.tiles_per_split < all ? first + g.tiles_per_split : all;
-    Acc acc;
+  static __device__ __forceinline__ void clear(Acc& acc) {
 #pragma unroll
     for (int q = 0; q < kPlanes; ++q)
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[q][i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    if constexpr (DIRECT) {
-      auto load = [&](int kt, short* to) {
-        const At w = at(g, kt);
-        issue<LA, BM, TA, false>(g, w, r0, g.m, to, tid);
-        issue<LB, BN, TB, true>(g, w, c0, g.n, to + BM * BK, tid);
-      };
-      if (first < last) load(first, lds);
+  }
+
+  static __device__ __forceinline__ void direct_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int tid, int wm, int wn, int lane) {
+    const uint32_t off_a = lane_offset<LA, BM, false>(g, tid), off_b = lane_offset<LB, BN, true>(g, tid);
+    const auto load = [&](int kt, short* to) {
+      const At w = at(g, kt);
+      issue<LA, BM, TA, false>(g, w, r0, off_a, to, tid);
+      issue<LB, BN, TB, true>(g, w, c0, off_b, to + kPlanes * BM * BK, tid);
+    };
+    const auto buffer = [&](int kt) { return lds + ((kt - first) & 1) * kTile; };
+    // Tile `kt` has arrived for all wavefronts, and none reads the one before it any more: the next one may take its place.
+    const auto advance = [&](int kt) {
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      if (kt + 1 < last) load(kt + 1, buffer(kt + 1));
+    };
+    if (first >= last) return;
+    load(first, buffer(first));
+    advance(first);
+    Frags f0, f1;
+    read(f0, buffer(first), 0, wm, wn, lane);
+    if constexpr (BK == 64) {
       for (int kt = first; kt < last; ++kt) {
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();  // this tile has arrived for all wavefronts, and nobody reads the other buffer any more
-        if (kt + 1 < last) load(kt + 1, lds + ((kt - first + 1) & 1) * kTile);
-        multiply(lds + ((kt - first) & 1) * kTile, acc, wm, wn, lane);
+        read(f1, buffer(kt), 32, wm, wn, lane);
+        multiply(acc, f0);
+        if (kt + 1 < last) {
+          advance(kt + 1);
+          read(f0, buffer(kt + 1), 0, wm, wn, lane);
+        }
+        multiply(acc, f1);
       }
     } else {
-      Elem8<DT> ra[TA], rb[TB];
-      auto load = [&](int kt) {
-        const At w = at(g, kt);
-        fetch<LA, BM, TA, false>(g, w, r0, g.m, ra, tid);
-        fetch<LB, BN, TB, true>(g, w, c0, g.n, rb, tid);
+      const auto turn = [&](int kt, const Frags& now, Frags& next) {
+        if (kt + 1 < last) {
+          advance(kt + 1);
+          read(next, buffer(kt + 1), 0, wm, wn, lane);
+        }
+        multiply(acc, now);
       };
-      auto put = [&](short* to) {
-        place<LA, BM, TA>(ra, to, tid);
-        place<LB, BN, TB>(rb, to + kPlanes * BM * BK, tid);
-      };
-      if (first < last) {
-        load(first);
-        put(lds);
+      int kt = first;
+      for (; kt + 2 < last; kt += 2) {
+        turn(kt, f0, f1);
+        turn(kt + 1, f1, f0);
       }
-      for (int kt = first; kt < last; ++kt) {
-        __syncthreads();
-        if (kt + 1 < last) load(kt + 1);
-        multiply(lds + ((kt - first) & 1) * kTile, acc, wm, wn, lane);
-        if (kt + 1 < last) put(lds + ((kt - first + 1) & 1) * kTile);
-      }
+      turn(kt, f0, f1);
+      if (kt + 1 < last) multiply(acc, f1);
     }
+  }
+
+  // Group kg of KG has tiles first + kg, first + kg + KG, ...
+  static __device__ __forceinline__ void staged_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int kg, int tid, int wm, int wn, int lane) {
+    Elem8<DT> ra[TA], rb[TB];
+    const auto load = [&](int kt) {
+      const At w = at(g, kt);
+      fetch<LA, BM, TA, false>(g, w, r0, g.m, ra, tid);
+      fetch<LB, BN, TB, true>(g, w, c0, g.n, rb, tid);
+    };
+    const auto put = [&](short* to) {
+      place<LA, BM, TA>(ra, to, tid);
+      place<LB, BN, TB>(rb, to + kPlanes * BM * BK, tid);
+    };
+    short* mine = lds + kg * 2 * kTile;
+    if (first + kg < last) {
+      load(first + kg);
+      put(mine);
+    }
+    int at = 0;
+    for (int kt = first; kt < last; kt += KG, at ^= 1) {
+      __syncthreads();
+      const int now = kt + kg, next = now + KG;
+      if (next < last) load(next);
+      if (now < last) {
+#pragma unroll
+        for (int k0 = 0; k0 < BK; k0 += 32) {
+          Frags f;
+          read(f, mine + at * kTile, k0, wm, wn, lane);
+          multiply(acc, f);
+        }
+      }
+      if (next < last) put(mine + (at ^ 1) * kTile);
+    }
+  }
+
+  static __device__ __forceinline__ void run(const GemmArgs& g, short* lds) {
+    const int tid = threadIdx.x % NT, lane = tid & 63;
+    const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WC, wn = wave % WC;
+    const int all = g.seg > 0 ? (g.seg + BK - 1) / BK * g.nseg : 0;
+    int t, first = 0, last = all;
+    float* partial = nullptr;
+    if ((int)blockIdx.x < g.whole) {
+      t = on_xcd(blockIdx.x, g.whole);
+    } else {
+      const int rest = g.tiles_m * g.tiles_n - g.whole;
+      const int lin = on_xcd((int)blockIdx.x - g.whole, rest * g.splits);
+      t = g.whole + lin / g.splits;
+      first = lin % g.splits * g.per_split;
+      last = first + g.per_split < all ? first + g.per_split : all;
+      partial = g.partial + (int64_t)lin * (BM * BN);
+    }
+    int tm, tn;
+    tile_of(g, t, tm, tn);
+    const int r0 = origin(tm * BM, g.m, BM, LA == KS), c0 = origin(tn * kCols, g.n, kCols, LB == KS);
+    Acc acc;
+    clear(acc);
+    if constexpr (DIRECT) direct_loop(g, acc, lds, r0, c0, first, last, tid, wm, wn, lane);
+    else staged_loop(g, acc, lds, r0, c0, first, last, kg, tid, wm, wn, lane);
     __syncthreads();
     if constexpr (kPlanes == 3) {
 #pragma unroll
@@ -428,39 +549,71 @@ struct Gemm {
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[0][i][j][e] = fmaf(fmaf(acc[2][i][j][e], 0.00390625f, acc[1][i][j][e]), 0.00390625f, acc[0][i][j][e]);
     }
-    finish(g, acc[0], (float*)lds + wave * kSlab, r0 + wm * FM * 16, c0 + wn * (EPI == kEpiGated ? FN * 8 : FN * 16), lane, split);
+    if constexpr (KG > 1) {  // the groups' sums, in their order
+      float* join = (float*)lds;
+      if (kg > 0) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) *(f32x4*)(join + (((kg - 1) * FM + i) * FN + j) * NT * 4 + tid * 4) = acc[0][i][j];
+      }
+      __syncthreads();
+      if (kg == 0) {
+#pragma unroll
+        for (int q = 0; q < KG - 1; ++q)
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[0][i][j] += *(const f32x4*)(join + ((q * FM + i) * FN + j) * NT * 4 + tid * 4);
+      }
+      __syncthreads();
+      if (kg > 0) return;
+    }
+    finish(g, acc[0], (float*)lds + wave * kSlab, tm, tn, r0, c0, wm, wn, lane, partial);
   }
 };
 
 template <typename G>
-__global__ __launch_bounds__(G::NT) void k_gemm(GemmArgs g) {
+__global__ __launch_bounds__(G::kThreads) void k_gemm(GemmArgs g) {
   __shared__ __attribute__((aligned(16))) short lds[G::kLdsBytes / 2];
   G::run(g, lds);
 }
 
-// The sums of a product whose k was split: eight columns of a row per thread, the splits in order, then the epilogue.
-template <int DT, int EPI>
+// The tiles of the result whose k was shared: eight columns of a row per thread, the shares in order, then the epilogue.
+template <typename G>
 __global__ __launch_bounds__(256) void k_join(GemmArgs g) {
-  const int64_t groups = (g.n + 7) / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t row = id / groups, col = (id - row * groups) * 8;
-  if (row >= g.m) return;
-  const int64_t width = EPI == kEpiGated ? 2 * (int64_t)g.n : g.n, left = g.n - col;
+  constexpr int kGroups = G::kCols / 8, kPer = G::BM * kGroups / 256;  // workgroups of a tile
+  const int tile = blockIdx.x / kPer, id = blockIdx.x % kPer * 256 + threadIdx.x;
+  int tm, tn;
+  tile_of(g, g.whole + tile, tm, tn);
+  const int in_row = id / kGroups, in_col = id % kGroups * 8;
+  const int64_t row = G::origin(tm * G::BM, g.m, G::BM, G::kAByK) + in_row;
+  int64_t col = G::origin(tn * G::kCols, g.n, G::kCols, G::kBByK) + in_col;
+  const int over = (int)(tn * G::kCols - col);
+  if (row >= g.m || row < tm * G::BM || col >= g.n || over >= 8) return;
   float v[8] = {}, u[8] = {};
   for (int s = 0; s < g.splits; ++s) {
-    const int64_t base = ((int64_t)s * g.m + row) * width + col;
-    float t[8];
-    load8<kFP32>(g.partial, base, left, t);
+    const float* p = g.partial + ((int64_t)tile * g.splits + s) * (G::BM * G::BN);
+    float x[8];
+    load8<kFP32>(p, in_row * G::BN + in_col, 8, x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += t[i];
-    if constexpr (EPI == kEpiGated) {
-      load8<kFP32>(g.partial, base + g.n, left, t);
+    for (int i = 0; i < 8; ++i) v[i] += x[i];
+    if constexpr (G::EPI == kEpiGated) {
+      load8<kFP32>(p, in_row * G::BN + G::kCols + in_col, 8, x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] += t[i];
+      for (int i = 0; i < 8; ++i) u[i] += x[i];
     }
   }
+  int count = 8;
+  if (over > 0) {
+    col += over;
+    count -= over;
+    drop_first(v, over);
+    if constexpr (G::EPI == kEpiGated) drop_first(u, over);
+  }
   ColumnState state;
-  epi_columns<EPI>(g, col, state);
-  epi_row<DT, EPI>(g, state, row, col, v, u);
+  epi_columns<G::EPI>(g, col, state);
+  epi_row<G::DT, G::EPI>(g, state, row, col, count, v, u);
 }
 
 }  // namespace layers

@@ -4,8 +4,8 @@
 namespace triaccel {
 namespace layers {
 
-hipError_t launch_gemm_fp32(Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t stream) {
-  return launch_any<kFP32>(kind, p, direct, g, stream);
+hipError_t launch_gemm_fp32(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream) {
+  return launch_any<kFP32>(kind, p, g, stream);
 }
 
 }  // namespace layers

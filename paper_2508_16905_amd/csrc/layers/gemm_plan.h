@@ -1,41 +1,75 @@
-// How a product is cut into workgroups: host side, from sizes alone.
+// How a product is cut into workgroups: host side, from sizes and the alignment of its operands alone.
 #pragma once
 #include <stdint.h>
 
 namespace triaccel {
 namespace layers {
 
+// S: 64 x 64, staged.  M: 128 x 128, L: 256 x 256, both straight to LDS.
 enum Tile : int { kTileS = 0, kTileM = 1, kTileL = 2 };
 
 struct GemmPlan {
-  int tile;
-  int32_t tiles_m, tiles_n, splits, tiles_per_split;
+  int tile, groups;         // groups: of wavefronts that share the k of a tile (S)
+  int32_t tiles_m, tiles_n, whole, splits, per_split;
   uint64_t partial_bytes;
+  double us;                // what the model below expects
 };
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// m x n results (gated: n columns of two products), k = nseg segments of seg.  `direct`: operands that can go straight to LDS.
-inline GemmPlan plan_gemm(bool fp32, bool gated, bool direct, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
+// The model, in microseconds: a workgroup computes a tile at a rate of its own, the card holds `slots` of them, and what is
+// left over after whole rounds of `slots` tiles is shared out over k where that is shorter (the sums then go through memory
+// and a second launch).
+inline GemmPlan plan_tile(int tile, bool fp32, bool gated, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
+  const int64_t half = gated ? 2 : 1, bk = fp32 ? 32 : 64;
+  const int64_t edge = tile == kTileL ? 256 : tile == kTileM ? 128 : 64;
   GemmPlan p{};
-  const int64_t half = gated ? 2 : 1;
-  const auto tiles = [&](int64_t edge) { return ceil_div(m, edge) * ceil_div(n * half, edge); };
-  p.tile = !fp32 && direct && tiles(256) >= 160 ? kTileL : tiles(128) >= 128 ? kTileM : kTileS;
-  const int64_t edge = p.tile == kTileL ? 256 : p.tile == kTileM ? 128 : 64;
+  p.tile = tile;
   p.tiles_m = (int32_t)ceil_div(m, edge);
   p.tiles_n = (int32_t)ceil_div(n * half, edge);
-  const int64_t k_tiles = seg > 0 ? ceil_div(seg, fp32 ? 32 : 64) * nseg : 1, all = (int64_t)p.tiles_m * p.tiles_n;
-  int64_t splits = 1;
-  if (all < 256 && k_tiles >= 8) {
-    splits = 512 / all;
-    if (splits > k_tiles / 4) splits = k_tiles / 4;
-    if (splits > 32) splits = 32;
-    if (splits < 1) splits = 1;
+  const int64_t k_tiles = seg > 0 ? ceil_div(seg, bk) * nseg : 1, all = (int64_t)p.tiles_m * p.tiles_n;
+  p.groups = tile == kTileS && k_tiles >= 4 && all <= 512 ? (fp32 ? 2 : 4) : 1;
+  // microseconds of a tile of k, and of what a workgroup has besides
+  const double per_k = tile == kTileL ? 0.95 : tile == kTileM ? (fp32 ? 1.3 : 0.75) : (fp32 ? 1.6 : 1.0) / p.groups, fixed = 5.0;
+  const int64_t slots = tile == kTileL ? 256 : tile == kTileM ? (fp32 ? 256 : 512) : p.groups > 1 ? 256 : 1024;
+  const int64_t rounds = all / slots, rest = all % slots;
+  const int64_t least = tile == kTileS ? 4 * p.groups : 4;  // tiles of k that a share has at least
+  p.whole = (int32_t)all;
+  p.splits = 1;
+  p.per_split = (int32_t)k_tiles;
+  p.us = (double)(rounds + (rest ? 1 : 0)) * (per_k * (double)k_tiles + fixed);
+  if (rest) {
+    int64_t s = slots / rest;
+    if (s > k_tiles / least) s = k_tiles / least;
+    if (s > 32) s = 32;
+    if (s > 1) {
+      const int64_t per = ceil_div(k_tiles, s);
+      const uint64_t bytes = (uint64_t)rest * (uint64_t)ceil_div(k_tiles, per) * (uint64_t)(edge * edge) * 4u;
+      const double us = (double)rounds * (per_k * (double)k_tiles + fixed) + per_k * (double)per + fixed + 7.0 + (double)bytes * 2.0 / 4.0e6;
+      if (us < p.us) {
+        p.us = us;
+        p.whole = (int32_t)(all - rest);
+        p.per_split = (int32_t)per;
+        p.splits = (int32_t)ceil_div(k_tiles, per);
+        p.partial_bytes = bytes;
+      }
+    }
   }
-  p.tiles_per_split = (int32_t)ceil_div(k_tiles, splits);
-  p.splits = (int32_t)ceil_div(k_tiles, p.tiles_per_split);
-  p.partial_bytes = p.splits > 1 ? (uint64_t)p.splits * (uint64_t)m * (uint64_t)(n * half) * 4u : 0;
   return p;
+}
+
+// m x n results (gated: n columns of two products), k = nseg segments of seg.  `pack_us`: what it takes to lay the operands out
+// for the direct form.
+inline GemmPlan plan_gemm(bool fp32, bool gated, double pack_us, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
+  GemmPlan best = plan_tile(kTileS, fp32, gated, m, n, seg, nseg);
+  for (int tile = kTileM; tile <= (fp32 ? kTileM : kTileL); ++tile) {
+    const int64_t edge = tile == kTileL ? 256 : 128;
+    // the direct form shifts its last tiles inwards: the result is no smaller than one of them
+    if (m < edge || n * (gated ? 2 : 1) < edge || seg < 1) continue;
+    const GemmPlan p = plan_tile(tile, fp32, gated, m, n, seg, nseg);
+    if (p.us + pack_us < best.us + (best.tile == kTileS ? 0.0 : pack_us)) best = p;
+  }
+  return best;
 }
 
 }  // namespace layers

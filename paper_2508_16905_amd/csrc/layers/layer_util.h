@@ -37,6 +37,53 @@ __device__ __forceinline__ Elem8<DT> load_raw8(const Elem<DT>* p, int64_t n) {
   for (int i = 0; i < 8; ++i) v[i] = i < n ? *as_global<Elem<DT>>(p + i) : (Elem<DT>)0.0f;
   return v;
 }
+// Elements at .. at + 7 of a row of `len` >= 1, zeros past its end, without a branch per lane: what ends the row is loaded
+// from eight before its end and moved down.
+__device__ __forceinline__ void move_down(uint32_t (&w)[4], int halves) {
+  const bool b4 = halves & 4, b2 = halves & 2, b1 = halves & 1;
+  if (halves >= 8) halves = 8;
+  w[0] = b4 ? w[2] : w[0]; w[1] = b4 ? w[3] : w[1]; w[2] = b4 ? 0u : w[2]; w[3] = b4 ? 0u : w[3];
+  w[0] = b2 ? w[1] : w[0]; w[1] = b2 ? w[2] : w[1]; w[2] = b2 ? w[3] : w[2]; w[3] = b2 ? 0u : w[3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t up = i < 3 ? w[i + 1] : 0u;
+    w[i] = b1 ? w[i] >> 16 | up << 16 : w[i];
+    w[i] = halves == 8 ? 0u : w[i];
+  }
+}
+template <int DT>
+__device__ __forceinline__ Elem8<DT> load_edge8(const Elem<DT>* row, int64_t at, int64_t len) {
+  Elem8<DT> v;
+  if (len >= 8) {
+    const int64_t from = at < len - 8 ? at : len - 8;
+    const int s = at - from < 8 ? (int)(at - from) : 8;
+    v = load_raw8<DT>(row + from);
+    if constexpr (DT == kFP32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = s & 4 ? (i < 4 ? v[i + 4 & 7] : 0.0f) : v[i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = s & 2 ? (i < 6 ? v[i + 2 & 7] : 0.0f) : v[i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = s & 1 ? (i < 7 ? v[i + 1 & 7] : 0.0f) : v[i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = s == 8 ? 0.0f : v[i];
+    } else {
+      typedef __attribute__((ext_vector_type(4))) uint32_t W;
+      W x = __builtin_bit_cast(W, v);
+      uint32_t w[4] = {x[0], x[1], x[2], x[3]};
+      move_down(w, s);
+      x = W{w[0], w[1], w[2], w[3]};
+      v = __builtin_bit_cast(Elem8<DT>, x);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const Elem<DT> e = *as_global<Elem<DT>>(row + (at + i < len ? at + i : len - 1));
+      v[i] = at + i < len ? e : (Elem<DT>)0.0f;
+    }
+  }
+  return v;
+}
 template <int DT>
 __device__ __forceinline__ void load8(const void* base, int64_t at, int64_t n, float (&out)[8]) {
   const Elem8<DT> v = load_raw8<DT>((const Elem<DT>*)base + at, n);
@@ -75,6 +122,25 @@ __device__ __forceinline__ void store1_of(int dtype, void* base, int64_t at, flo
   if (dtype == kFP32) as_global<float>(base)[at] = v;
   else if (dtype == kBF16) as_global<__bf16>(base)[at] = narrow<kBF16>(v);
   else as_global<_Float16>(base)[at] = narrow<kFP16>(v);
+}
+
+// ---- fp32 in three parts, for the matrix cores (gemm.h) ---
+// Rounded to bf16; cut off instead where rounding would make an infinity of a number.
+__device__ __forceinline__ uint32_t part_bits(float x) {
+  const uint32_t b = f32_to_bf16_bits(x);
+  return (b & 0x7fffu) == 0x7f80u ? f2u(x) >> 16 : b;
+}
+// fp32 -> three bf16 parts.  A rest is below 2^120 and its multiple below 2^128; what is not finite has no rest.
+__device__ __forceinline__ void split3(const Elem8<kFP32>& v, s16x8 (&out)[3]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t h = part_bits(v[i]);
+    const float r = __builtin_isfinite(v[i]) ? (v[i] - bf16_bits_to_f32(h)) * 256.0f : 0.0f;
+    const uint32_t m = part_bits(r);
+    out[0][i] = (short)h;
+    out[1][i] = (short)m;
+    out[2][i] = (short)part_bits((r - bf16_bits_to_f32(m)) * 256.0f);
+  }
 }
 
 // ---- activations ------------------------------------------------------------------------------------------------

@@ -13,9 +13,23 @@ struct Drop;
 
 enum Product : int { kForward = 0, kGatedForward = 1, kInputGrad = 2, kWeightGrad = 3 };
 
-hipError_t launch_gemm_fp16(Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t stream);
-hipError_t launch_gemm_bf16(Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t stream);
-hipError_t launch_gemm_fp32(Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t stream);
+hipError_t launch_gemm_fp16(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream);
+hipError_t launch_gemm_bf16(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream);
+hipError_t launch_gemm_fp32(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream);
+
+// Matrices laid out for the direct form of a product: rows of whole 16-byte units, zeros behind `cols`; fp32 as three bf16 parts,
+// `plane` elements apart.
+struct PackedMatrix {
+  const void* src;
+  int64_t ld, rows, cols;
+  void* dst;
+  int64_t dst_ld, plane;
+};
+struct PackArgs {
+  PackedMatrix m[4];
+  int32_t count;
+};
+hipError_t launch_pack(int dtype, const PackArgs& a, hipStream_t stream);
 
 // The gradient before the activation, and its sums over the rows.
 struct SlopeArgs {

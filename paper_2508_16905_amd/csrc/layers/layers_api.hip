@@ -91,90 +91,177 @@ uint64_t padded(uint64_t bytes) { return (bytes + 255u) & ~(uint64_t)255u; }
 
 // ---- products ------------------------------------------------------------------------------------------------------
 
-hipError_t run_product(int32_t dtype, Product kind, const GemmPlan& p, bool direct, const GemmArgs& g, hipStream_t s) {
-  return dtype == TRIACCEL_FP16 ? launch_gemm_fp16(kind, p, direct, g, s)
-         : dtype == TRIACCEL_BF16 ? launch_gemm_bf16(kind, p, direct, g, s) : launch_gemm_fp32(kind, p, direct, g, s);
+hipError_t run_product(int32_t dtype, Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t s) {
+  return dtype == TRIACCEL_FP16 ? launch_gemm_fp16(kind, p, g, s)
+         : dtype == TRIACCEL_BF16 ? launch_gemm_bf16(kind, p, g, s) : launch_gemm_fp32(kind, p, g, s);
 }
 
-// Whether an operand's 16-byte units can go straight to LDS: units whole and aligned (`whole`: the contiguous length ends with a
-// unit, or its rows have room for the last), and a tile's rows within 31 bits of its first.
-bool direct_ok(const void* p, int64_t ld, bool whole) {
-  return whole && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0 && ld < (1 << 21);
+// An operand as the caller (or the workspace) has it.  `room`: its rows may be read up to a whole unit of eight, zeros.
+struct Operand {
+  const void* p;
+  int64_t ld, rows, cols;
+  bool room;
+};
+// Whether its 16-byte units can go straight to LDS as they lie: whole, aligned, a tile's rows within 31 bits of its first.
+bool as_it_lies(int32_t dtype, const Operand& o) {
+  return dtype != TRIACCEL_FP32 && (o.room || o.cols % 8 == 0) && (reinterpret_cast<uintptr_t>(o.p) & 15u) == 0 && o.ld % 8 == 0 && o.ld < (1 << 21);
 }
-GemmPlan plan_of(int32_t dtype, Product kind, bool direct, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
-  return plan_gemm(dtype == TRIACCEL_FP32, kind == kGatedForward, direct, m, n, seg, nseg);
+int64_t packed_ld(const Operand& o) { return (o.cols + 7) / 8 * 8; }
+uint64_t packed_bytes(int32_t dtype, const Operand& o) {
+  return padded((uint64_t)o.rows * (uint64_t)packed_ld(o) * (dtype == TRIACCEL_FP32 ? 6u : 2u));
 }
-// The workspace does not depend on alignment: the larger of both plans.
-uint64_t partial_bytes(int32_t dtype, Product kind, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
-  const uint64_t a = plan_of(dtype, kind, true, m, n, seg, nseg).partial_bytes, b = plan_of(dtype, kind, false, m, n, seg, nseg).partial_bytes;
-  return padded(a > b ? a : b);
+
+// Up to three operands (the second matrix of a gated block among them) and up to two products of them, planned together:
+// what is laid out anew is laid out once.
+struct Products {
+  int32_t dtype;
+  int count;
+  Operand op[4];       // dz, weight, second weight, x; p NULL = not there
+  bool pack[4];
+  uint64_t at[4];      // in the workspace
+  uint64_t partial, total;
+};
+// The two weights of a gated block are read with one stride: both as they lie, or both anew.
+bool in_place(const Products& q, int i) {
+  if (i == 1 || i == 2) return as_it_lies(q.dtype, q.op[1]) && (!q.op[2].rows || as_it_lies(q.dtype, q.op[2]));
+  return as_it_lies(q.dtype, q.op[i]);
+}
+// `need`: bit i = a direct product reads operand i.
+void lay_out(Products& q, uint64_t from, unsigned need, uint64_t partial_bytes) {
+  uint64_t at = from;
+  for (int i = 0; i < 4; ++i) {
+    q.pack[i] = (need >> i & 1u) && q.op[i].rows > 0 && !in_place(q, i);
+    q.at[i] = at;
+    if (q.pack[i]) at += packed_bytes(q.dtype, q.op[i]);
+  }
+  q.partial = at;
+  q.total = at + padded(partial_bytes);
+}
+// What laying out the operands in `need` costs, in the plan's microseconds; more than anything where it cannot be done.
+double pack_us(const Products& q, unsigned need) {
+  uint64_t bytes = 0;
+  for (int i = 0; i < 4; ++i) {
+    if (!(need >> i & 1u)) continue;
+    // a tile's rows lie within 31 bits, and one launch lays everything out
+    if (q.op[i].cols >= (1 << 21) || q.op[i].rows * q.op[i].cols >= (int64_t)1 << 32) return 1e30;
+    if (!in_place(q, i)) bytes += 2 * packed_bytes(q.dtype, q.op[i]);
+  }
+  return bytes ? 6.0 + (double)bytes / 4.0e6 : 0.0;
+}
+int pack(const Products& q, char* ws, hipStream_t s) {
+  PackArgs a{};
+  for (int i = 0; i < 4; ++i)
+    if (q.pack[i]) {
+      const Operand& o = q.op[i];
+      a.m[a.count++] = PackedMatrix{o.p, o.ld, o.rows, o.cols, ws + q.at[i], packed_ld(o), o.rows * packed_ld(o)};
+    }
+  return a.count ? hip_status(launch_pack(q.dtype, a, s), "operands laid out") : TRIACCEL_OK;
+}
+// Operand i for a product: as it was laid out if the product is direct.
+const void* place(const Products& q, int i, bool direct, char* ws, int64_t& ld, int64_t& plane) {
+  const bool anew = direct && q.pack[i];
+  ld = anew ? packed_ld(q.op[i]) : q.op[i].ld;
+  plane = anew ? q.op[i].rows * ld : 0;
+  return anew ? ws + q.at[i] : q.op[i].p;
+}
+
+struct ForwardPlan {
+  Products q;
+  GemmPlan g;
+};
+ForwardPlan plan_forward(int32_t dtype, Product kind, int64_t rows, int64_t in, int64_t out, const void* x, int64_t ldx, const void* w, const void* w2, int64_t ldw) {
+  ForwardPlan f{};
+  f.q.dtype = dtype;
+  const bool two = kind == kGatedForward;
+  f.q.op[1] = Operand{w, ldw, out, in, false};
+  if (two) f.q.op[2] = Operand{w2, ldw, out, in, false};
+  f.q.op[3] = Operand{x, ldx, rows, in, false};
+  unsigned need = two ? 14u : 10u;
+  f.g = plan_gemm(dtype == TRIACCEL_FP32, two, pack_us(f.q, need), rows, out, in, 1);
+  if (f.g.tile == kTileS) need = 0;
+  lay_out(f.q, 0, need, f.g.partial_bytes);
+  return f;
 }
 
 // ---- gradients before the activation ---------------------------------------------------------------------------------
 
-struct BackwardLayout {
-  int64_t width;
-  uint64_t dz, sums, partial, total;
+struct BackwardPlan {
+  int64_t width;            // columns of dz in the workspace, a whole number of units
+  uint64_t sums, total;     // dz is at 0
   int32_t blocks;
   int64_t rows_per_block;
+  Products q;
+  GemmPlan dx, dw;
 };
-// `dz_needed`: dz is not dy itself.  `wide`: 2 for the gated block.
-BackwardLayout backward_layout(int32_t dtype, int64_t rows, int64_t in, int64_t out, bool dz_needed, bool sums, bool dx, bool dw, int64_t wide) {
-  BackwardLayout l{};
-  l.width = (out + 7) / 8 * 8;
+struct BackwardShape {
+  int32_t dtype;
+  int64_t rows, in, out, wide;  // wide: 2 for the gated block
+  bool slope, sums, dx, dw;     // slope: dz is not dy itself
+  const void *dy, *x, *w, *w2;
+  int64_t lddy, ldx, ldw;
+};
+BackwardPlan plan_backward(const BackwardShape& b, const void* ws) {
+  BackwardPlan l{};
+  l.width = (b.out + 7) / 8 * 8;
   // 64 rows a workgroup, more where that makes over 128 blocks (their sums are added up by one workgroup per 64 columns)
   l.rows_per_block = 64;
-  if (ceil_div(rows, l.rows_per_block) > 128) l.rows_per_block = ceil_div(rows, 128);
-  l.blocks = (int32_t)ceil_div(rows, l.rows_per_block);
-  l.dz = 0;
-  l.sums = dz_needed ? padded((uint64_t)rows * (uint64_t)(wide * l.width) * (uint64_t)bytes_of(dtype)) : 0;
-  l.partial = l.sums + (sums ? padded((uint64_t)l.blocks * (uint64_t)(wide * out) * 4u) : 0);
-  const uint64_t a = dx ? partial_bytes(dtype, kInputGrad, rows, in, out, wide) : 0;
-  const uint64_t b = dw ? partial_bytes(dtype, kWeightGrad, wide == 2 ? l.width + out : out, in, rows, 1) : 0;
-  l.total = l.partial + (a > b ? a : b);
+  if (ceil_div(b.rows, l.rows_per_block) > 128) l.rows_per_block = ceil_div(b.rows, 128);
+  l.blocks = (int32_t)ceil_div(b.rows, l.rows_per_block);
+  l.sums = b.slope ? padded((uint64_t)b.rows * (uint64_t)(b.wide * l.width) * (uint64_t)bytes_of(b.dtype)) : 0;
+  const uint64_t from = l.sums + (b.sums ? padded((uint64_t)l.blocks * (uint64_t)(b.wide * b.out) * 4u) : 0);
+  Products& q = l.q;
+  q.dtype = b.dtype;
+  q.op[0] = b.slope ? Operand{ws, b.wide * l.width, b.rows, b.wide * l.width, true} : Operand{b.dy, b.lddy, b.rows, b.out, false};
+  q.op[1] = Operand{b.w, b.ldw, b.out, b.in, false};
+  if (b.wide == 2) q.op[2] = Operand{b.w2, b.ldw, b.out, b.in, false};
+  q.op[3] = Operand{b.x, b.ldx, b.rows, b.in, false};
+  const bool fp32 = b.dtype == TRIACCEL_FP32;
+  unsigned need_dx = b.wide == 2 ? 7u : 3u, need_dw = 9u, need = 0;
+  uint64_t partial = 0;
+  if (b.dx && b.rows > 0) {
+    l.dx = plan_gemm(fp32, false, pack_us(q, need_dx), b.rows, b.in, b.out, b.wide);
+    if (l.dx.tile != kTileS) need |= need_dx;
+    partial = l.dx.partial_bytes;
+  }
+  if (b.dw) {
+    l.dw = plan_gemm(fp32, false, pack_us(q, need_dw & ~need), b.wide == 2 ? l.width + b.out : b.out, b.in, b.rows, 1);
+    if (l.dw.tile != kTileS) need |= need_dw;
+    if (l.dw.partial_bytes > partial) partial = l.dw.partial_bytes;
+  }
+  lay_out(q, from, need, partial);
+  l.total = q.total;
   return l;
 }
 
-// dx = dz W (gated: dg Wg + du Wu) and dW = dz^T x from dz as it lies (ld: its rows' distance; gated: du `step` behind dg).
-struct BackwardProducts {
-  int32_t dtype;
-  int64_t rows, in, out;
-  const void *dz;
-  int64_t ld, step;
-  bool dz_padded;
-  const void *x, *w, *w2;
-  int64_t ldx, ldw;
+// dx = dz W (gated: dg Wg + du Wu) and dW = dz^T x.
+struct BackwardOut {
   void *dx, *dw, *dw2;
   int64_t lddx, lddw;
   int32_t dw_dtype;
-  float* partial;
 };
-int backward_products(const BackwardProducts& q, hipStream_t s) {
-  const int64_t wide = q.w2 || q.dw2 ? 2 : 1;
-  if (q.dx && q.rows > 0) {
-    const bool direct = q.dtype != TRIACCEL_FP32 && direct_ok(q.dz, q.ld, q.dz_padded || q.out % 8 == 0) && q.step % 8 == 0 &&
-                        direct_ok(q.w, q.ldw, q.in % 8 == 0) && (!q.w2 || direct_ok(q.w2, q.ldw, true));
-    const GemmPlan p = plan_of(q.dtype, kInputGrad, direct, q.rows, q.in, q.out, wide);
+int backward_products(const BackwardShape& b, const BackwardPlan& l, const BackwardOut& o, char* ws, hipStream_t s) {
+  TA_TRY(pack(l.q, ws, s));
+  if (b.dx && b.rows > 0) {
+    const bool direct = l.dx.tile != kTileS;
     GemmArgs g{};
-    g.a = q.dz; g.lda = q.ld; g.b = q.w; g.b2 = q.w2; g.ldb = q.ldw;
-    g.m = (int32_t)q.rows; g.n = (int32_t)q.in; g.seg = (int32_t)q.out; g.nseg = (int32_t)wide; g.seg_step = (int32_t)q.step;
-    g.partial = q.partial;
-    g.c = q.dx; g.ldc = q.lddx; g.crows = g.csplit = 0x7fffffff; g.c_fp32 = q.dtype == TRIACCEL_FP32;
-    TA_TRY(hip_status(run_product(q.dtype, kInputGrad, p, direct, g, s), "gradient of the input"));
+    g.a = place(l.q, 0, direct, ws, g.lda, g.a_plane);
+    g.b = place(l.q, 1, direct, ws, g.ldb, g.b_plane);
+    if (b.wide == 2) g.b2 = place(l.q, 2, direct, ws, g.ldb, g.b_plane);
+    g.m = (int32_t)b.rows; g.n = (int32_t)b.in; g.seg = (int32_t)b.out; g.nseg = (int32_t)b.wide; g.seg_step = (int32_t)l.width;
+    g.partial = (float*)(ws + l.q.partial);
+    g.c = o.dx; g.ldc = o.lddx; g.crows = g.csplit = 0x7fffffff; g.c_fp32 = b.dtype == TRIACCEL_FP32;
+    TA_TRY(hip_status(run_product(b.dtype, kInputGrad, l.dx, g, s), "gradient of the input"));
   }
-  if (q.dw) {
-    // no rows: the product has no terms and its result is zero
-    const bool direct = q.dtype != TRIACCEL_FP32 && direct_ok(q.dz, q.ld, q.dz_padded || q.out % 8 == 0) && q.step % 8 == 0 &&
-                        direct_ok(q.x, q.ldx, q.in % 8 == 0);
-    const int64_t m = wide == 2 ? q.step + q.out : q.out;
-    const GemmPlan p = plan_of(q.dtype, kWeightGrad, direct, m, q.in, q.rows, 1);
+  if (b.dw) {  // no rows: the product has no terms and its result is zero
+    const bool direct = l.dw.tile != kTileS;
     GemmArgs g{};
-    g.a = q.dz; g.lda = q.ld; g.b = q.x; g.ldb = q.ldx;
-    g.m = (int32_t)m; g.n = (int32_t)q.in; g.seg = (int32_t)q.rows; g.nseg = 1;
-    g.partial = q.partial;
-    g.c = q.dw; g.c2 = q.dw2; g.ldc = q.lddw; g.crows = (int32_t)q.out; g.csplit = wide == 2 ? (int32_t)q.step : 0x7fffffff;
-    g.c_fp32 = q.dw_dtype == TRIACCEL_FP32;
-    TA_TRY(hip_status(run_product(q.dtype, kWeightGrad, p, direct, g, s), "gradient of the weights"));
+    g.a = place(l.q, 0, direct, ws, g.lda, g.a_plane);
+    g.b = place(l.q, 3, direct, ws, g.ldb, g.b_plane);
+    g.m = (int32_t)(b.wide == 2 ? l.width + b.out : b.out); g.n = (int32_t)b.in; g.seg = (int32_t)b.rows; g.nseg = 1;
+    g.partial = (float*)(ws + l.q.partial);
+    g.c = o.dw; g.c2 = o.dw2; g.ldc = o.lddw; g.crows = (int32_t)b.out; g.csplit = b.wide == 2 ? (int32_t)l.width : 0x7fffffff;
+    g.c_fp32 = o.dw_dtype == TRIACCEL_FP32;
+    TA_TRY(hip_status(run_product(b.dtype, kWeightGrad, l.dw, g, s), "gradient of the weights"));
   }
   return TRIACCEL_OK;
 }
@@ -212,6 +299,16 @@ int check_gated_backward(const triaccel_gated_backward_args* a) {
   if (a->dweight_dtype != a->dtype && a->dweight_dtype != TRIACCEL_FP32)
     return refuse(TRIACCEL_E_BAD_DTYPE, "dweight_dtype is neither the call's dtype nor FP32");
   return check_act(a->act, false);
+}
+
+BackwardShape shape_of(const triaccel_linear_backward_args& a) {
+  const bool products = a.dx || a.dweight;
+  return BackwardShape{a.dtype, a.rows, a.in, a.out, 1, slope_needed(a) && products, a.dbias != nullptr, a.dx != nullptr, a.dweight != nullptr,
+                       a.dy, a.x, a.weight, nullptr, a.lddy, a.ldx, a.ldw};
+}
+BackwardShape shape_of(const triaccel_gated_backward_args& a) {
+  return BackwardShape{a.dtype, a.rows, a.in, a.out, 2, a.dx || a.dw_gate, a.db_gate != nullptr, a.dx != nullptr, a.dw_gate != nullptr,
+                       a.dh, a.x, a.w_gate, a.w_up, a.lddh, a.ldx, a.ldw};
 }
 
 // ---- norms -----------------------------------------------------------------------------------------------------------
@@ -259,7 +356,7 @@ extern "C" {
 
 int64_t triaccel_linear_workspace(const triaccel_linear_args* a) {
   TA_TRY(check_linear(a));
-  return a->rows ? (int64_t)partial_bytes(a->dtype, kForward, a->rows, a->out, a->in, 1) : 0;
+  return a->rows ? (int64_t)plan_forward(a->dtype, kForward, a->rows, a->in, a->out, a->x, a->ldx, a->weight, nullptr, a->ldw).q.total : 0;
 }
 
 int triaccel_linear(const triaccel_linear_args* a, void* hip_stream) {
@@ -270,24 +367,27 @@ int triaccel_linear(const triaccel_linear_args* a, void* hip_stream) {
   if (a->residual) TA_TRY(check_matrix(a->residual, a->ldr, a->rows, a->out, a->dtype, "residual"));
   TA_TRY(check_matrix(a->y, a->ldy, a->rows, a->out, a->dtype, "y"));
   if (a->pre) TA_TRY(check_matrix(a->pre, a->ldpre, a->rows, a->out, a->dtype, "pre"));
-  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, (uint64_t)triaccel_linear_workspace(a)));
   if (a->rows == 0) return TRIACCEL_OK;
-  const bool direct = a->dtype != TRIACCEL_FP32 && direct_ok(a->x, a->ldx, a->in % 8 == 0) && direct_ok(a->weight, a->ldw, true);
-  const GemmPlan p = plan_of(a->dtype, kForward, direct, a->rows, a->out, a->in, 1);
+  const ForwardPlan f = plan_forward(a->dtype, kForward, a->rows, a->in, a->out, a->x, a->ldx, a->weight, nullptr, a->ldw);
+  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, f.q.total));
+  char* ws = (char*)a->workspace;
+  TA_TRY(pack(f.q, ws, (hipStream_t)hip_stream));
+  const bool direct = f.g.tile != kTileS;
   GemmArgs g{};
-  g.a = a->x; g.lda = a->ldx; g.b = a->weight; g.ldb = a->ldw;
+  g.a = place(f.q, 3, direct, ws, g.lda, g.a_plane);
+  g.b = place(f.q, 1, direct, ws, g.ldb, g.b_plane);
   g.m = (int32_t)a->rows; g.n = (int32_t)a->out; g.seg = (int32_t)a->in; g.nseg = 1;
-  g.partial = (float*)a->workspace;
+  g.partial = (float*)(ws + f.q.partial);
   g.c = a->y; g.ldc = a->ldy; g.pre = a->pre; g.ldpre = a->ldpre;
   g.bias = a->bias; g.bias_dtype = a->bias_dtype; g.act = a->act;
   g.residual = a->residual; g.ldr = a->ldr;
   g.drop = drop_of(a->drop, a->scale);
-  return hip_status(run_product(a->dtype, kForward, p, direct, g, (hipStream_t)hip_stream), "linear");
+  return hip_status(run_product(a->dtype, kForward, f.g, g, (hipStream_t)hip_stream), "linear");
 }
 
 int64_t triaccel_linear_backward_workspace(const triaccel_linear_backward_args* a) {
   TA_TRY(check_linear_backward(a));
-  return (int64_t)backward_layout(a->dtype, a->rows, a->in, a->out, slope_needed(*a) && (a->dx || a->dweight), a->dbias, a->dx, a->dweight, 1).total;
+  return (int64_t)plan_backward(shape_of(*a), a->workspace).total;
 }
 
 int triaccel_linear_backward(const triaccel_linear_backward_args* a, void* hip_stream) {
@@ -299,8 +399,9 @@ int triaccel_linear_backward(const triaccel_linear_backward_args* a, void* hip_s
   if (a->dx) TA_TRY(check_matrix(a->dx, a->lddx, a->rows, a->in, a->dtype, "dx"));
   if (a->dweight) TA_TRY(check_matrix(a->dweight, a->lddw, a->out, a->in, a->dweight_dtype, "dweight"));
   TA_TRY(check_vector(a->dbias, a->dbias_dtype, "dbias"));
-  const bool slope = slope_needed(*a) && (a->dx || a->dweight);
-  const BackwardLayout l = backward_layout(a->dtype, a->rows, a->in, a->out, slope, a->dbias, a->dx, a->dweight, 1);
+  const BackwardShape b = shape_of(*a);
+  const bool slope = b.slope;
+  const BackwardPlan l = plan_backward(b, a->workspace);
   TA_TRY(check_workspace(a->workspace, a->workspace_bytes, l.total));
   char* ws = (char*)a->workspace;
   hipStream_t s = (hipStream_t)hip_stream;
@@ -309,7 +410,7 @@ int triaccel_linear_backward(const triaccel_linear_backward_args* a, void* hip_s
     SlopeArgs q{};
     q.dy = a->dy; q.lddy = a->lddy; q.gate = a->pre; q.ldg = a->ldpre;
     q.rows = a->rows; q.cols = a->out; q.width = l.width;
-    q.dz = slope ? ws + l.dz : nullptr;
+    q.dz = slope ? ws : nullptr;
     q.sums = a->dbias ? (float*)(ws + l.sums) : nullptr;
     q.rows_per_block = l.rows_per_block; q.blocks = l.blocks; q.act = a->act; q.drop = &drop;
     TA_TRY(hip_status(launch_slope(a->dtype, false, q, s), "gradient before the activation"));
@@ -318,18 +419,12 @@ int triaccel_linear_backward(const triaccel_linear_backward_args* a, void* hip_s
     ColumnSums c{(const float*)(ws + l.sums), a->out, a->out, l.blocks, 1, a->dbias_dtype, {a->dbias}};
     TA_TRY(hip_status(launch_column_sums(c, s), "gradient of the bias"));
   }
-  BackwardProducts q{};
-  q.dtype = a->dtype; q.rows = a->rows; q.in = a->in; q.out = a->out;
-  q.dz = slope ? (const void*)(ws + l.dz) : a->dy; q.ld = slope ? l.width : a->lddy; q.dz_padded = slope;
-  q.x = a->x; q.ldx = a->ldx; q.w = a->weight; q.ldw = a->ldw;
-  q.dx = a->dx; q.lddx = a->lddx; q.dw = a->dweight; q.lddw = a->lddw; q.dw_dtype = a->dweight_dtype;
-  q.partial = (float*)(ws + l.partial);
-  return backward_products(q, s);
+  return backward_products(b, l, BackwardOut{a->dx, a->dweight, nullptr, a->lddx, a->lddw, a->dweight_dtype}, ws, s);
 }
 
 int64_t triaccel_gated_workspace(const triaccel_gated_args* a) {
   TA_TRY(check_gated(a));
-  return a->rows ? (int64_t)partial_bytes(a->dtype, kGatedForward, a->rows, a->out, a->in, 1) : 0;
+  return a->rows ? (int64_t)plan_forward(a->dtype, kGatedForward, a->rows, a->in, a->out, a->x, a->ldx, a->w_gate, a->w_up, a->ldw).q.total : 0;
 }
 
 int triaccel_gated(const triaccel_gated_args* a, void* hip_stream) {
@@ -346,23 +441,26 @@ int triaccel_gated(const triaccel_gated_args* a, void* hip_stream) {
     TA_TRY(check_matrix(a->gate, a->ldg, a->rows, a->out, a->dtype, "gate"));
     TA_TRY(check_matrix(a->up, a->ldg, a->rows, a->out, a->dtype, "up"));
   }
-  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, (uint64_t)triaccel_gated_workspace(a)));
   if (a->rows == 0) return TRIACCEL_OK;
-  const bool direct = a->dtype != TRIACCEL_FP32 && direct_ok(a->x, a->ldx, a->in % 8 == 0) && direct_ok(a->w_gate, a->ldw, true) &&
-                      direct_ok(a->w_up, a->ldw, true);
-  const GemmPlan p = plan_of(a->dtype, kGatedForward, direct, a->rows, a->out, a->in, 1);
+  const ForwardPlan f = plan_forward(a->dtype, kGatedForward, a->rows, a->in, a->out, a->x, a->ldx, a->w_gate, a->w_up, a->ldw);
+  TA_TRY(check_workspace(a->workspace, a->workspace_bytes, f.q.total));
+  char* ws = (char*)a->workspace;
+  TA_TRY(pack(f.q, ws, (hipStream_t)hip_stream));
+  const bool direct = f.g.tile != kTileS;
   GemmArgs g{};
-  g.a = a->x; g.lda = a->ldx; g.b = a->w_gate; g.b2 = a->w_up; g.ldb = a->ldw;
+  g.a = place(f.q, 3, direct, ws, g.lda, g.a_plane);
+  g.b = place(f.q, 1, direct, ws, g.ldb, g.b_plane);
+  g.b2 = place(f.q, 2, direct, ws, g.ldb, g.b_plane);
   g.m = (int32_t)a->rows; g.n = (int32_t)a->out; g.seg = (int32_t)a->in; g.nseg = 1;
-  g.partial = (float*)a->workspace;
+  g.partial = (float*)(ws + f.q.partial);
   g.c = a->h; g.ldc = a->ldh; g.pre = a->gate; g.pre2 = a->up; g.ldpre = a->ldg;
   g.bias = a->b_gate; g.bias2 = a->b_up; g.bias_dtype = a->bias_dtype; g.act = a->act;
-  return hip_status(run_product(a->dtype, kGatedForward, p, direct, g, (hipStream_t)hip_stream), "gated");
+  return hip_status(run_product(a->dtype, kGatedForward, f.g, g, (hipStream_t)hip_stream), "gated");
 }
 
 int64_t triaccel_gated_backward_workspace(const triaccel_gated_backward_args* a) {
   TA_TRY(check_gated_backward(a));
-  return (int64_t)backward_layout(a->dtype, a->rows, a->in, a->out, a->dx || a->dw_gate, a->db_gate, a->dx, a->dw_gate, 2).total;
+  return (int64_t)plan_backward(shape_of(*a), a->workspace).total;
 }
 
 int triaccel_gated_backward(const triaccel_gated_backward_args* a, void* hip_stream) {
@@ -384,16 +482,16 @@ int triaccel_gated_backward(const triaccel_gated_backward_args* a, void* hip_str
   }
   TA_TRY(check_vector(a->db_gate, a->dbias_dtype, "db_gate"));
   TA_TRY(check_vector(a->db_up, a->dbias_dtype, "db_up"));
-  const bool products = a->dx || a->dw_gate;
-  const BackwardLayout l = backward_layout(a->dtype, a->rows, a->in, a->out, products, a->db_gate, a->dx, a->dw_gate, 2);
+  const BackwardShape b = shape_of(*a);
+  const BackwardPlan l = plan_backward(b, a->workspace);
   TA_TRY(check_workspace(a->workspace, a->workspace_bytes, l.total));
   char* ws = (char*)a->workspace;
   hipStream_t s = (hipStream_t)hip_stream;
-  if ((products || a->db_gate) && a->rows > 0) {
+  if ((b.slope || a->db_gate) && a->rows > 0) {
     SlopeArgs q{};
     q.dy = a->dh; q.lddy = a->lddh; q.gate = a->gate; q.up = a->up; q.ldg = a->ldg;
     q.rows = a->rows; q.cols = a->out; q.width = l.width;
-    q.dz = products ? ws + l.dz : nullptr;
+    q.dz = b.slope ? ws : nullptr;
     q.sums = a->db_gate ? (float*)(ws + l.sums) : nullptr;
     q.rows_per_block = l.rows_per_block; q.blocks = l.blocks; q.act = a->act;
     TA_TRY(hip_status(launch_slope(a->dtype, true, q, s), "gradients before the activation"));
@@ -402,13 +500,7 @@ int triaccel_gated_backward(const triaccel_gated_backward_args* a, void* hip_str
     ColumnSums c{(const float*)(ws + l.sums), a->out, 2 * a->out, l.blocks, 2, a->dbias_dtype, {a->db_gate, a->db_up}};
     TA_TRY(hip_status(launch_column_sums(c, s), "gradients of the biases"));
   }
-  BackwardProducts q{};
-  q.dtype = a->dtype; q.rows = a->rows; q.in = a->in; q.out = a->out;
-  q.dz = ws + l.dz; q.ld = 2 * l.width; q.step = l.width; q.dz_padded = true;
-  q.x = a->x; q.ldx = a->ldx; q.w = a->w_gate; q.w2 = a->w_up; q.ldw = a->ldw;
-  q.dx = a->dx; q.lddx = a->lddx; q.dw = a->dw_gate; q.dw2 = a->dw_up; q.lddw = a->lddw; q.dw_dtype = a->dweight_dtype;
-  q.partial = (float*)(ws + l.partial);
-  return backward_products(q, s);
+  return backward_products(b, l, BackwardOut{a->dx, a->dw_gate, a->dw_up, a->lddx, a->lddw, a->dweight_dtype}, ws, s);
 }
 
 int triaccel_residual_norm(const triaccel_residual_norm_args* a, void* hip_stream) {

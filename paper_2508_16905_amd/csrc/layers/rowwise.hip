@@ -100,6 +100,34 @@ __global__ __launch_bounds__(1024) void k_column_sums(ColumnSums a) {
   }
 }
 
+// Eight elements of a row per lane, all matrices in one launch.
+template <int DT>
+__global__ __launch_bounds__(256) void k_pack(PackArgs a) {
+  int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const PackedMatrix& m = a.m[i];
+    const int64_t units = m.dst_ld / 8, all = m.rows * units;
+    if (i >= a.count) return;
+    if (id >= all) {
+      id -= all;
+      continue;
+    }
+    const int64_t row = all >> 32 ? id / units : (int64_t)((uint32_t)id / (uint32_t)units), col = (id - row * units) * 8;
+    const Elem8<DT> v = load_edge8<DT>((const Elem<DT>*)m.src + row * m.ld, col, m.cols);
+    short* dst = (short*)m.dst + row * m.dst_ld + col;
+    if constexpr (DT == kFP32) {
+      s16x8 part[3];
+      split3(v, part);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) *(TA_GLOBAL s16x8*)(dst + q * m.plane) = part[q];
+    } else {
+      *(TA_GLOBAL s16x8*)dst = __builtin_bit_cast(s16x8, v);
+    }
+    return;
+  }
+}
+
 // Eight elements per lane; a wavefront has 512 neighbouring columns of one row.
 template <int DT>
 __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a, Drop drop, int64_t per_row) {
@@ -132,6 +160,16 @@ hipError_t launch_slope(int dtype, bool gated, const SlopeArgs& a, hipStream_t s
   if (dtype == kFP16) go(std::integral_constant<int, kFP16>());
   else if (dtype == kBF16) go(std::integral_constant<int, kBF16>());
   else go(std::integral_constant<int, kFP32>());
+  return hipGetLastError();
+}
+
+hipError_t launch_pack(int dtype, const PackArgs& a, hipStream_t stream) {
+  int64_t threads = 0;
+  for (int i = 0; i < a.count; ++i) threads += a.m[i].rows * (a.m[i].dst_ld / 8);
+  const dim3 grid((uint32_t)ceil_div(threads, 256));
+  if (dtype == kFP16) k_pack<kFP16><<<grid, 256, 0, stream>>>(a);
+  else if (dtype == kBF16) k_pack<kBF16><<<grid, 256, 0, stream>>>(a);
+  else k_pack<kFP32><<<grid, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
