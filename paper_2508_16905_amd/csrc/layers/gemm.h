@@ -250,8 +250,8 @@ struct Gemm {
       return (uint32_t)(k * ld + unit * 8) * 2u;
     }
   }
-  template <int L, int R, int T, bool IS_B>
-  static __device__ __forceinline__ void issue(const GemmArgs& g, const At& w, int r0, uint32_t off, short* tile, int tid) {
+  template <int L, int R, int T, bool IS_B, bool FULL>
+  static __device__ __forceinline__ void issue(const GemmArgs& g, const At& w, int r0, uint32_t off, short* tile, int tid, int wave) {
     const int64_t ld = IS_B ? g.ldb : g.lda, plane = IS_B ? g.b_plane : g.a_plane;
     const int64_t koff = (IS_B ? 0 : (int64_t)w.seg * g.seg_step) + w.k0;
     const int64_t skip = L == KC ? (int64_t)r0 * ld + koff : koff * ld + r0;
@@ -259,10 +259,9 @@ struct Gemm {
     const char* p1 = (const char*)((const E*)g.b2 + skip);
     constexpr int kStep = L == KC ? NT / (BK / 8) : NT / (R / 8);  // rows, or k, from one t to the next
     static_assert(kStep % 16 == 0 || (L == KC && kStep % 8 == 0), "the exchange of units is the same for all t");
-    const bool full = w.left >= BK;
     uint32_t id = (uint32_t)tid;
-    if (!full) asm volatile("" : "+v"(id));  // what follows from it is not worth registers throughout the loop
-    // 0 inside the operand's k, else where the unit's zeros are
+    if constexpr (!FULL) asm volatile("" : "+v"(id));  // what follows from it is not worth registers throughout the loop
+    // whether unit t NT + tid is past the end of k: its zeros come from elsewhere
     const auto outside = [&](int t) {
       if constexpr (L == KC) return (int)(tile_unit<KC, R, BK>((int)id / (BK / 8), (int)id % (BK / 8)) % (BK / 8)) * 8 >= w.left;
       else return (int)id / (R / 8) + t * kStep >= w.left;
@@ -272,23 +271,25 @@ struct Gemm {
       const char* base = p0;
       int64_t step = t * kStep * ld * 2;
       if constexpr (EPI == kEpiGated && IS_B && L == KC) {
-        // rows t kStep ... of the tile, all in one matrix for a wavefront: kStep and its 8 or 16 rows divide kHalf's
-        bool second;
-        const int wave_row = (int)__builtin_amdgcn_readfirstlane((uint32_t)tid) / (BK / 8);
+        // a wavefront's rows are all of one matrix; its lanes' offsets were made from the rows that t = 0 has
+        const int wave_row = wave * 64 / (BK / 8);
+        bool second, ignored;
         const int row = b_row(t * kStep + wave_row, second);
-        if (second) base = p1;
-        step = (row - wave_row) * ld * 2;
-        // the lane's offset was made from b_row(row of tid), which is wave_row plus the same as here
-        bool ignored;
-        step += (wave_row - b_row(wave_row, ignored)) * ld * 2;
+        base = second ? p1 : p0;
+        step = (row - b_row(wave_row, ignored)) * ld * 2;
       }
 #pragma unroll
       for (int q = 0; q < kPlanes; ++q) {
-        const char* src = base + step + q * plane * 2 + off;
-        if (!full) src = outside(t) ? (const char*)kZeroPage : src;
         // lane i's 16 bytes go to the wavefront's place plus 16 i
-        __builtin_amdgcn_global_load_lds((const TA_GLOBAL char*)src,
-                                         (__attribute__((address_space(3))) char*)tile + q * R * BK * 2 + (t * NT + (tid & ~63)) * 16, 16, 0, 0);
+        const auto to = (__attribute__((address_space(3))) char*)tile + q * R * BK * 2 + (t * NT + wave * 64) * 16;
+        const char* from = base + q * plane * 2;
+        if constexpr (FULL) {
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, 0x7fffffff, kBufferRaw), to, 16,
+                                                   (int)off, (int)step, 0, 0);
+        } else {
+          const char* src = outside(t) ? (const char*)kZeroPage : from + step + off;
+          __builtin_amdgcn_global_load_lds((const TA_GLOBAL char*)src, to, 16, 0, 0);
+        }
       }
     }
   }
@@ -435,50 +436,88 @@ struct Gemm {
         for (int j = 0; j < FN; ++j) acc[q][i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  static __device__ __forceinline__ void direct_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int tid, int wm, int wn, int lane) {
+  // The order in which a stage's instructions are issued: reads of LDS and loads (a group of each) before each quarter of the
+  // products, so that the matrix cores have work while the next fragments and tiles are on their way.  Left alone the
+  // compiler puts all reads first and all products last.
+  template <int LOADS>
+  static __device__ __forceinline__ void interleave() {
+    constexpr int kParts = 4, kMfma = (kPlanes == 3 ? 6 : 1) * FM * FN;
+    constexpr int kReads = kPlanes * (FM * (LA == KS ? 2 : 1) + FN * (LB == KS ? 2 : 1));
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, kMfma / kParts / 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kParts - 1) / kParts, 0);
+      if constexpr (LOADS > 0) __builtin_amdgcn_sched_group_barrier(0x020, (LOADS + kParts - 1) / kParts, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kMfma / kParts - kMfma / kParts / 2, 0);
+    }
+  }
+
+  static __device__ __forceinline__ void direct_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int tid, int wave, int wm, int wn, int lane) {
     const uint32_t off_a = lane_offset<LA, BM, false>(g, tid), off_b = lane_offset<LB, BN, true>(g, tid);
-    const auto load = [&](int kt, short* to) {
-      const At w = at(g, kt);
-      issue<LA, BM, TA, false>(g, w, r0, off_a, to, tid);
-      issue<LB, BN, TB, true>(g, w, c0, off_b, to + kPlanes * BM * BK, tid);
-    };
     const auto buffer = [&](int kt) { return lds + ((kt - first) & 1) * kTile; };
-    // Tile `kt` has arrived for all wavefronts, and none reads the one before it any more: the next one may take its place.
-    const auto advance = [&](int kt) {
+    const auto load = [&](int kt, auto full) {
+      constexpr bool kFull = decltype(full)::value;
+      const At w = at(g, kt);
+      short* to = buffer(kt);
+      issue<LA, BM, TA, false, kFull>(g, w, r0, off_a, to, tid, wave);
+      issue<LB, BN, TB, true, kFull>(g, w, c0, off_b, to + kPlanes * BM * BK, tid, wave);
+    };
+    // What was sent to LDS has arrived for all wavefronts, and what they read before is in their registers.
+    const auto meet = [&]() {
+      __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_waitcnt(0);
       __syncthreads();
-      if (kt + 1 < last) load(kt + 1, buffer(kt + 1));
+      __builtin_amdgcn_sched_barrier(0);
     };
-    if (first >= last) return;
-    load(first, buffer(first));
-    advance(first);
-    Frags f0, f1;
-    read(f0, buffer(first), 0, wm, wn, lane);
-    if constexpr (BK == 64) {
-      for (int kt = first; kt < last; ++kt) {
-        read(f1, buffer(kt), 32, wm, wn, lane);
-        multiply(acc, f0);
-        if (kt + 1 < last) {
-          advance(kt + 1);
-          read(f0, buffer(kt + 1), 0, wm, wn, lane);
+    const auto whole = [&](int kt) { return kt < last && at(g, kt).left >= BK; };
+    constexpr int kLoads = kPlanes * (TA + TB);
+    int sent = first;  // the last tile sent for
+    if (first < last) load(first, std::false_type());
+    for (int kt = first; kt < last;) {
+      if (sent == kt && whole(kt + 1) && whole(kt + 2)) {
+        Frags f0, f1;
+        meet();
+        load(kt + 1, std::true_type());
+        read(f0, buffer(kt), 0, wm, wn, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (BK == 64) {
+          for (; whole(kt + 2); ++kt) {
+            read(f1, buffer(kt), 32, wm, wn, lane);
+            multiply(acc, f0);
+            interleave<0>();
+            meet();
+            load(kt + 2, std::true_type());
+            read(f0, buffer(kt + 1), 0, wm, wn, lane);
+            multiply(acc, f1);
+            interleave<kLoads>();
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        } else {
+          const auto turn = [&](int t, Frags& now, Frags& next) {
+            meet();
+            load(t + 2, std::true_type());
+            read(next, buffer(t + 1), 0, wm, wn, lane);
+            multiply(acc, now);
+            interleave<kLoads>();
+            __builtin_amdgcn_sched_barrier(0);
+          };
+          for (; whole(kt + 2) && whole(kt + 3); kt += 2) {
+            turn(kt, f0, f1);
+            turn(kt + 1, f1, f0);
+          }
         }
-        multiply(acc, f1);
+        sent = kt + 1;
       }
-    } else {
-      const auto turn = [&](int kt, const Frags& now, Frags& next) {
-        if (kt + 1 < last) {
-          advance(kt + 1);
-          read(next, buffer(kt + 1), 0, wm, wn, lane);
-        }
-        multiply(acc, now);
-      };
-      int kt = first;
-      for (; kt + 2 < last; kt += 2) {
-        turn(kt, f0, f1);
-        turn(kt + 1, f1, f0);
+      // one by one: the last tiles, and those around the end of a segment
+      meet();
+      if (sent == kt && kt + 1 < last) load(++sent, std::false_type());
+#pragma unroll 1
+      for (int k0 = 0; k0 < BK; k0 += 32) {
+        Frags f;
+        read(f, buffer(kt), k0, wm, wn, lane);
+        multiply(acc, f);
       }
-      turn(kt, f0, f1);
-      if (kt + 1 < last) multiply(acc, f1);
+      ++kt;
     }
   }
 
@@ -538,7 +577,7 @@ struct Gemm {
     const int r0 = origin(tm * BM, g.m, BM, LA == KS), c0 = origin(tn * kCols, g.n, kCols, LB == KS);
     Acc acc;
     clear(acc);
-    if constexpr (DIRECT) direct_loop(g, acc, lds, r0, c0, first, last, tid, wm, wn, lane);
+    if constexpr (DIRECT) direct_loop(g, acc, lds, r0, c0, first, last, tid, wave, wm, wn, lane);
     else staged_loop(g, acc, lds, r0, c0, first, last, kg, tid, wm, wn, lane);
     __syncthreads();
     if constexpr (kPlanes == 3) {
