@@ -11,10 +11,9 @@
 // products the six largest are summed, those of one scale in one accumulator; what is dropped is at most 2^-26 of a product.
 // Six bf16 products have 2.6 times the rate of the fp32 matrix instructions (2.5 PFLOP/s / 6 = 417 and 157 TFLOP/s).
 //
-// Two forms.  DIRECT: operands of whole, aligned 16-byte units (fp32: their parts, laid out by k_pack) go from memory to LDS
-// without registers, a tile ahead, while the fragments of the next 32 k are read from LDS beside the products of these.
-// Staged: any strides, alignment and sizes through registers, with fp32 split on the way; for small products, where what counts
-// is the number of launches, and where KG groups of wavefronts share the k of one tile.
+// Two forms.  WIDE: a tile ahead in registers, fragments of the next 32 k ahead of these products, any strides and alignment
+// (fp32: the operands' parts, laid out by k_pack); the result has the size of a tile at least.  Staged: small tiles, any
+// sizes, with fp32 split on the way; for small products, where KG groups of wavefronts share the k of one tile.
 #pragma once
 #include <type_traits>
 
@@ -32,7 +31,7 @@ struct GemmArgs {
   int32_t m, n;             // rows and columns of the result (kEpiGated: n columns from each of b and b2)
   int32_t seg, nseg;        // k = nseg segments of `seg`
   int32_t seg_step;         // where segment 1 of A (KC) begins
-  int64_t a_plane, b_plane; // fp32, DIRECT: elements between the parts
+  int64_t a_plane, b_plane; // fp32, wide: elements between the parts
   int32_t tiles_m, tiles_n;
   int32_t whole;            // the first `whole` tiles of the result have a workgroup each, the others `splits`, of
   int32_t splits, per_split;  // `per_split` tiles of k
@@ -49,8 +48,6 @@ struct GemmArgs {
   int32_t bias_dtype, act;
   Drop drop;
 };
-
-__device__ const uint32_t kZeroPage[4] = {0, 0, 0, 0};
 
 // ---- epilogue of eight columns of one row ------------------------------------------------------------------------
 struct ColumnState {
@@ -177,9 +174,8 @@ __device__ __forceinline__ int on_xcd(int id, int total) {
   return xcd * per + (xcd < more ? xcd : more) + (id >> 3);
 }
 
-template <int DT_, int LA, int LB, int BM_, int BN_, int WR, int WC, int KG, int EPI_, bool DIRECT>
+template <int DT_, int LA, int LB, int BM_, int BN_, int WR, int WC, int KG, int EPI_, bool WIDE>
 struct Gemm {
-  static constexpr bool kAByK = LA == KS, kBByK = LB == KS;
   static constexpr int DT = DT_, BM = BM_, BN = BN_, EPI = EPI_;
   static constexpr int kPlanes = DT == kFP32 ? 3 : 1;
   static constexpr int BK = DT == kFP32 ? 32 : 64;
@@ -199,16 +195,15 @@ struct Gemm {
   static constexpr int kCols = EPI == kEpiGated ? BN / 2 : BN;
   static_assert(TA >= 1 && TB >= 1 && kAUnits % NT == 0 && kBUnits % NT == 0, "whole units per thread");
   static_assert(EPI != kEpiGated || FN % 2 == 0, "half of a wavefront's columns from each matrix");
-  static_assert(!DIRECT || KG == 1, "groups are for the staged form");
-  typedef typename std::conditional<DIRECT, __bf16, Elem<DT>>::type E;  // DIRECT: any 16 bits
+  static_assert(!WIDE || KG == 1, "groups are for the staged form");
+  typedef typename std::conditional<WIDE, __bf16, Elem<DT>>::type E;  // WIDE: any 16 bits
   typedef f32x4 Acc[kPlanes][FM][FN];  // [q]: what counts 2^-8q
 
-  // Where the tile of the result begins whose first row is `r0`, and likewise for columns.  DIRECT: the last tile begins
+  // Where the tile of the result begins whose first row is `r0`, and likewise for columns.  WIDE: the last tile begins
   // earlier, so that it lies inside (the plan has m >= BM and n >= kCols); what the one before it has is not stored twice.
-  static __device__ __forceinline__ int origin(int r0, int rows, int size, bool whole_units) {
-    if (!DIRECT) return r0;
-    const int last = (whole_units ? (rows + 7) & ~7 : rows) - size;
-    return r0 < last ? r0 : last;
+  static __device__ __forceinline__ int origin(int r0, int rows, int size) {
+    if (!WIDE) return r0;
+    return r0 < rows - size ? r0 : rows - size;
   }
 
   // Row of B (0 .. BN - 1) -> its matrix and row there.  With two matrices each wavefront has as many rows of the one as of
@@ -235,63 +230,82 @@ struct Gemm {
     return At{s, k0, g.seg - k0};
   }
 
-  // --- straight to LDS ---
-  // The tile lies inside the operand (see origin), so that unit t NT + tid is at a distance from unit tid that all lanes have in
+  // --- wide form ---
+  // A tile lies inside the operand (see origin), so that unit t NT + tid is at a distance from unit tid that all lanes have in
   // common: one offset per lane, the rest in scalar registers.
   template <int L, int R, bool IS_B>
   static __device__ __forceinline__ uint32_t lane_offset(const GemmArgs& g, int tid) {
     const int ld = (int)(IS_B ? g.ldb : g.lda);
     if constexpr (L == KC) {
-      const int row = tid / (BK / 8), unit = tile_unit<KC, R, BK>(row, tid % (BK / 8)) % (BK / 8);
       bool second;
-      return (uint32_t)((IS_B ? b_row(row, second) : row) * ld + unit * 8) * 2u;
+      const int row = tid / (BK / 8);
+      return (uint32_t)((IS_B ? b_row(row, second) : row) * ld + tid % (BK / 8) * 8) * 2u;
     } else {
-      const int k = tid / (R / 8), unit = tile_unit<KS, R, BK>(k, tid % (R / 8)) % (R / 8);
-      return (uint32_t)(k * ld + unit * 8) * 2u;
+      return (uint32_t)(tid / (R / 8) * ld + tid % (R / 8) * 8) * 2u;
     }
   }
-  template <int L, int R, int T, bool IS_B, bool FULL>
-  static __device__ __forceinline__ void issue(const GemmArgs& g, const At& w, int r0, uint32_t off, short* tile, int tid, int wave) {
-    const int64_t ld = IS_B ? g.ldb : g.lda, plane = IS_B ? g.b_plane : g.a_plane;
-    const int64_t koff = (IS_B ? 0 : (int64_t)w.seg * g.seg_step) + w.k0;
-    const int64_t skip = L == KC ? (int64_t)r0 * ld + koff : koff * ld + r0;
-    const char* p0 = (const char*)((const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a) + skip);
-    const char* p1 = (const char*)((const E*)g.b2 + skip);
+  // Where unit t of a tile of the operand begins (lane offsets aside), part q of fp32.
+  template <int L, int R, bool IS_B>
+  static __device__ __forceinline__ const char* unit_base(const GemmArgs& g, const At& w, int r0, int t, int q, int wave) {
     constexpr int kStep = L == KC ? NT / (BK / 8) : NT / (R / 8);  // rows, or k, from one t to the next
-    static_assert(kStep % 16 == 0 || (L == KC && kStep % 8 == 0), "the exchange of units is the same for all t");
-    uint32_t id = (uint32_t)tid;
-    if constexpr (!FULL) asm volatile("" : "+v"(id));  // what follows from it is not worth registers throughout the loop
-    // whether unit t NT + tid is past the end of k: its zeros come from elsewhere
-    const auto outside = [&](int t) {
-      if constexpr (L == KC) return (int)(tile_unit<KC, R, BK>((int)id / (BK / 8), (int)id % (BK / 8)) % (BK / 8)) * 8 >= w.left;
-      else return (int)id / (R / 8) + t * kStep >= w.left;
-    };
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const char* base = p0;
-      int64_t step = t * kStep * ld * 2;
-      if constexpr (EPI == kEpiGated && IS_B && L == KC) {
-        // a wavefront's rows are all of one matrix; its lanes' offsets were made from the rows that t = 0 has
-        const int wave_row = wave * 64 / (BK / 8);
-        bool second, ignored;
-        const int row = b_row(t * kStep + wave_row, second);
-        base = second ? p1 : p0;
-        step = (row - b_row(wave_row, ignored)) * ld * 2;
-      }
-#pragma unroll
-      for (int q = 0; q < kPlanes; ++q) {
-        // lane i's 16 bytes go to the wavefront's place plus 16 i
-        const auto to = (__attribute__((address_space(3))) char*)tile + q * R * BK * 2 + (t * NT + wave * 64) * 16;
-        const char* from = base + q * plane * 2;
-        if constexpr (FULL) {
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, 0x7fffffff, kBufferRaw), to, 16,
-                                                   (int)off, (int)step, 0, 0);
-        } else {
-          const char* src = outside(t) ? (const char*)kZeroPage : from + step + off;
-          __builtin_amdgcn_global_load_lds((const TA_GLOBAL char*)src, to, 16, 0, 0);
-        }
-      }
+    const int64_t ld = IS_B ? g.ldb : g.lda;
+    const int64_t koff = (IS_B ? 0 : (int64_t)w.seg * g.seg_step) + w.k0;
+    const E* p = (const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a);
+    int64_t step = t * kStep;
+    if constexpr (EPI == kEpiGated && IS_B && L == KC) {
+      // a wavefront's rows are all of one matrix; its lanes' offsets were made from the rows that t = 0 has
+      const int wave_row = wave * 64 / (BK / 8);
+      bool second, ignored;
+      const int row = b_row(t * kStep + wave_row, second);
+      if (second) p = (const E*)g.b2;
+      step = row - b_row(wave_row, ignored);
     }
+    const int64_t skip = (L == KC ? (int64_t)r0 * ld + koff : koff * ld + r0) + step * ld + q * (IS_B ? g.b_plane : g.a_plane);
+    return (const char*)(p + skip);
+  }
+  template <int L, int R, bool IS_B>
+  static __device__ __forceinline__ s16x8 get(const GemmArgs& g, const At& w, int r0, int t, int q, uint32_t off, int wave) {
+    typedef s16x8 __attribute__((aligned(2))) U;
+    return *(const TA_GLOBAL U*)(unit_base<L, R, IS_B>(g, w, r0, t, q, wave) + off);
+  }
+  // The same where the tile may pass the end of k: loaded from inside (the plan has seg >= 8) and, once it has arrived, moved
+  // to its place, zeros behind.
+  template <int L, int R, bool IS_B>
+  static __device__ __forceinline__ s16x8 get_edge(const GemmArgs& g, const At& w, int r0, int t, int q, int tid) {
+    const int slot = t * NT + tid;
+    const int64_t ld = IS_B ? g.ldb : g.lda;
+    const E* p = (const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a) + (IS_B ? 0 : (int64_t)w.seg * g.seg_step) * (L == KC ? 1 : ld);
+    const E* from;
+    if constexpr (L == KC) {
+      bool second = false;
+      const int row = IS_B ? b_row(slot / (BK / 8), second) : slot / (BK / 8), k = w.k0 + slot % (BK / 8) * 8;
+      from = (second ? (const E*)g.b2 : p) + (r0 + row) * ld + (k < g.seg - 8 ? k : g.seg - 8);
+    } else {
+      const int k = slot / (R / 8);
+      from = p + (w.k0 + (k < w.left ? k : 0)) * ld + r0 + slot % (R / 8) * 8;
+    }
+    typedef s16x8 __attribute__((aligned(2))) U;
+    return *(const TA_GLOBAL U*)(from + q * (IS_B ? g.b_plane : g.a_plane));
+  }
+  template <int L, int R>
+  static __device__ __forceinline__ s16x8 in_place(const GemmArgs& g, const At& w, s16x8 v, int t, int tid) {
+    const int slot = t * NT + tid;
+    if constexpr (L == KC) {
+      const int past = w.k0 + slot % (BK / 8) * 8 - (g.seg - 8);
+      typedef __attribute__((ext_vector_type(4))) uint32_t W;
+      const W x = __builtin_bit_cast(W, v);
+      uint32_t y[4] = {x[0], x[1], x[2], x[3]};
+      move_down(y, past > 0 ? past : 0);
+      return __builtin_bit_cast(s16x8, W{y[0], y[1], y[2], y[3]});
+    } else {
+      return slot / (R / 8) < w.left ? v : s16x8{};
+    }
+  }
+  template <int L, int R>
+  static __device__ __forceinline__ void put(short* tile, int t, int q, s16x8 v, int tid) {
+    const int slot = t * NT + tid;
+    const int u = L == KC ? tile_unit<KC, R, BK>(slot / (BK / 8), slot % (BK / 8)) : tile_unit<KS, R, BK>(slot / (R / 8), slot % (R / 8));
+    *(s16x8*)(tile + q * R * BK + 8 * u) = v;
   }
 
   // --- through registers ---
@@ -355,10 +369,11 @@ struct Gemm {
 #pragma unroll
       for (int q = 0; q < kPlanes; ++q) f.a[i][q] = fragment<LA, BM, BK>(tile + q * BM * BK, wm * FM * 16 + i * 16, k0, lane);
   }
+  template <int I0, int I1>
   static __device__ __forceinline__ void multiply(Acc& acc, const Frags& f) {
     // B first: a lane then has four neighbouring columns of one row of the result
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int i = I0; i < I1; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         const s16x8 *a = f.a[i], *b = f.b[j];
@@ -414,7 +429,7 @@ struct Gemm {
             if constexpr (EPI == kEpiGated) store8<kFP32>(partial, base + kCols, 8, u);
           } else {
             int count = 8;
-            if (DIRECT && over > 0) {
+            if (WIDE && over > 0) {
               count -= over;
               drop_first(v, over);
               if constexpr (EPI == kEpiGated) drop_first(u, over);
@@ -436,87 +451,140 @@ struct Gemm {
         for (int j = 0; j < FN; ++j) acc[q][i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // The order in which a stage's instructions are issued: reads of LDS and loads (a group of each) before each quarter of the
-  // products, so that the matrix cores have work while the next fragments and tiles are on their way.  Left alone the
-  // compiler puts all reads first and all products last.
-  template <int LOADS>
+  // What this wavefront wrote to LDS and read from it is done; then so it is for all wavefronts.  Loads from memory stay in
+  // flight.
+  static __device__ __forceinline__ void meet() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // The order in which a stage's instructions are issued: reads of LDS first, then what goes to it and the loads that take its
+  // place in the registers, each behind some products, so that the matrix cores have work meanwhile.  Left alone the compiler
+  // puts all reads first and all products last.
+  template <int READS, int WRITES, int MFMA>
   static __device__ __forceinline__ void interleave() {
-    constexpr int kParts = 4, kMfma = (kPlanes == 3 ? 6 : 1) * FM * FN;
-    constexpr int kReads = kPlanes * (FM * (LA == KS ? 2 : 1) + FN * (LB == KS ? 2 : 1));
+    constexpr int kEach = MFMA / (READS + 2 * WRITES + 1) > 0 ? MFMA / (READS + 2 * WRITES + 1) : 1;
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, kMfma / kParts / 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, (kReads + kParts - 1) / kParts, 0);
-      if constexpr (LOADS > 0) __builtin_amdgcn_sched_group_barrier(0x020, (LOADS + kParts - 1) / kParts, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, kMfma / kParts - kMfma / kParts / 2, 0);
+    for (int i = 0; i < READS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
+#pragma unroll
+    for (int i = 0; i < WRITES; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+      __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, MFMA, 0);
   }
 
-  static __device__ __forceinline__ void direct_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int tid, int wave, int wm, int wn, int lane) {
+  // Two tiles in LDS.  While tile kt is worked on from one, what was loaded of kt + 1 goes into the other and kt + 2 is sent
+  // for; the fragments of the next 32 k are read beside the products of these.
+  static __device__ __forceinline__ void wide_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int tid, int wave, int wm, int wn, int lane) {
+    if (first >= last) return;
     const uint32_t off_a = lane_offset<LA, BM, false>(g, tid), off_b = lane_offset<LB, BN, true>(g, tid);
     const auto buffer = [&](int kt) { return lds + ((kt - first) & 1) * kTile; };
-    const auto load = [&](int kt, auto full) {
-      constexpr bool kFull = decltype(full)::value;
+    const auto whole = [&](int kt) { return kt < last && at(g, kt).left >= BK; };
+    s16x8 ra[TA][kPlanes], rb[TB][kPlanes];
+    const auto fetch = [&](int kt) {
+      const At w = at(g, kt);
+      int id = tid;
+      asm volatile("" : "+v"(id));  // what follows from it is not worth registers throughout the loop
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q) {
+#pragma unroll
+        for (int t = 0; t < TA; ++t) ra[t][q] = get_edge<LA, BM, false>(g, w, r0, t, q, id);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) rb[t][q] = get_edge<LB, BN, true>(g, w, c0, t, q, id);
+      }
+    };
+    const auto store = [&](int kt) {
       const At w = at(g, kt);
       short* to = buffer(kt);
-      issue<LA, BM, TA, false, kFull>(g, w, r0, off_a, to, tid, wave);
-      issue<LB, BN, TB, true, kFull>(g, w, c0, off_b, to + kPlanes * BM * BK, tid, wave);
+      int id = tid;
+      asm volatile("" : "+v"(id));
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q) {
+#pragma unroll
+        for (int t = 0; t < TA; ++t) put<LA, BM>(to, t, q, in_place<LA, BM>(g, w, ra[t][q], t, id), id);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) put<LB, BN>(to + kPlanes * BM * BK, t, q, in_place<LB, BN>(g, w, rb[t][q], t, id), id);
+      }
     };
-    // What was sent to LDS has arrived for all wavefronts, and what they read before is in their registers.
-    const auto meet = [&]() {
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-      __builtin_amdgcn_sched_barrier(0);
+    // tile kt + 1 from the registers to LDS, tile kt + 2, a whole one, into them
+    const auto pass_on = [&](int kt) {
+      const At w = at(g, kt + 2);
+      short* to = buffer(kt + 1);
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q) {
+#pragma unroll
+        for (int t = 0; t < TA; ++t) {
+          put<LA, BM>(to, t, q, ra[t][q], tid);
+          ra[t][q] = get<LA, BM, false>(g, w, r0, t, q, off_a, wave);
+        }
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+          put<LB, BN>(to + kPlanes * BM * BK, t, q, rb[t][q], tid);
+          rb[t][q] = get<LB, BN, true>(g, w, c0, t, q, off_b, wave);
+        }
+      }
     };
-    const auto whole = [&](int kt) { return kt < last && at(g, kt).left >= BK; };
-    constexpr int kLoads = kPlanes * (TA + TB);
-    int sent = first;  // the last tile sent for
-    if (first < last) load(first, std::false_type());
-    for (int kt = first; kt < last;) {
-      if (sent == kt && whole(kt + 1) && whole(kt + 2)) {
+    constexpr int kMfma = (kPlanes == 3 ? 6 : 1) * FM * FN, kWrites = kPlanes * (TA + TB);
+    constexpr int kReads = kPlanes * (FM * (LA == KS ? 2 : 1) + FN * (LB == KS ? 2 : 1));
+    fetch(first);
+    store(first);
+    if (first + 1 < last) fetch(first + 1);
+    meet();
+    for (int kt = first; kt < last;) {  // tile kt is in LDS, tile kt + 1 on its way to the registers
+      if (whole(kt + 1) && whole(kt + 2) && (BK == 64 || whole(kt + 3))) {
         Frags f0, f1;
-        meet();
-        load(kt + 1, std::true_type());
         read(f0, buffer(kt), 0, wm, wn, lane);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (BK == 64) {
-          for (; whole(kt + 2); ++kt) {
+          do {
             read(f1, buffer(kt), 32, wm, wn, lane);
-            multiply(acc, f0);
-            interleave<0>();
+            pass_on(kt);
+            multiply<0, FM>(acc, f0);
+            interleave<kReads, kWrites, kMfma>();
             meet();
-            load(kt + 2, std::true_type());
             read(f0, buffer(kt + 1), 0, wm, wn, lane);
-            multiply(acc, f1);
-            interleave<kLoads>();
+            multiply<0, FM>(acc, f1);
+            interleave<kReads, 0, kMfma>();
             __builtin_amdgcn_sched_barrier(0);
-          }
+            ++kt;
+          } while (whole(kt + 2));
         } else {
-          const auto turn = [&](int t, Frags& now, Frags& next) {
+          const auto turn = [&](Frags& now, Frags& next) {
+            pass_on(kt);
+            multiply<0, FM / 2>(acc, now);
+            interleave<0, kWrites, kMfma / 2>();
             meet();
-            load(t + 2, std::true_type());
-            read(next, buffer(t + 1), 0, wm, wn, lane);
-            multiply(acc, now);
-            interleave<kLoads>();
+            read(next, buffer(kt + 1), 0, wm, wn, lane);
+            multiply<FM / 2, FM>(acc, now);
+            interleave<kReads, 0, kMfma / 2>();
             __builtin_amdgcn_sched_barrier(0);
+            ++kt;
           };
-          for (; whole(kt + 2) && whole(kt + 3); kt += 2) {
-            turn(kt, f0, f1);
-            turn(kt + 1, f1, f0);
-          }
+          do {
+            turn(f0, f1);
+            turn(f1, f0);
+          } while (whole(kt + 2) && whole(kt + 3));
         }
-        sent = kt + 1;
       }
       // one by one: the last tiles, and those around the end of a segment
-      meet();
-      if (sent == kt && kt + 1 < last) load(++sent, std::false_type());
+      if (kt + 1 < last) store(kt + 1);
+      if (kt + 2 < last) fetch(kt + 2);
 #pragma unroll 1
       for (int k0 = 0; k0 < BK; k0 += 32) {
         Frags f;
         read(f, buffer(kt), k0, wm, wn, lane);
-        multiply(acc, f);
+        multiply<0, FM>(acc, f);
       }
+      meet();
       ++kt;
     }
   }
@@ -529,14 +597,14 @@ struct Gemm {
       fetch<LA, BM, TA, false>(g, w, r0, g.m, ra, tid);
       fetch<LB, BN, TB, true>(g, w, c0, g.n, rb, tid);
     };
-    const auto put = [&](short* to) {
+    const auto put_all = [&](short* to) {
       place<LA, BM, TA>(ra, to, tid);
       place<LB, BN, TB>(rb, to + kPlanes * BM * BK, tid);
     };
     short* mine = lds + kg * 2 * kTile;
     if (first + kg < last) {
       load(first + kg);
-      put(mine);
+      put_all(mine);
     }
     int at = 0;
     for (int kt = first; kt < last; kt += KG, at ^= 1) {
@@ -548,10 +616,10 @@ struct Gemm {
         for (int k0 = 0; k0 < BK; k0 += 32) {
           Frags f;
           read(f, mine + at * kTile, k0, wm, wn, lane);
-          multiply(acc, f);
+          multiply<0, FM>(acc, f);
         }
       }
-      if (next < last) put(mine + (at ^ 1) * kTile);
+      if (next < last) put_all(mine + (at ^ 1) * kTile);
     }
   }
 
@@ -574,10 +642,10 @@ struct Gemm {
     }
     int tm, tn;
     tile_of(g, t, tm, tn);
-    const int r0 = origin(tm * BM, g.m, BM, LA == KS), c0 = origin(tn * kCols, g.n, kCols, LB == KS);
+    const int r0 = origin(tm * BM, g.m, BM), c0 = origin(tn * kCols, g.n, kCols);
     Acc acc;
     clear(acc);
-    if constexpr (DIRECT) direct_loop(g, acc, lds, r0, c0, first, last, tid, wave, wm, wn, lane);
+    if constexpr (WIDE) wide_loop(g, acc, lds, r0, c0, first, last, tid, wave, wm, wn, lane);
     else staged_loop(g, acc, lds, r0, c0, first, last, kg, tid, wm, wn, lane);
     __syncthreads();
     if constexpr (kPlanes == 3) {
@@ -626,8 +694,8 @@ __global__ __launch_bounds__(256) void k_join(GemmArgs g) {
   int tm, tn;
   tile_of(g, g.whole + tile, tm, tn);
   const int in_row = id / kGroups, in_col = id % kGroups * 8;
-  const int64_t row = G::origin(tm * G::BM, g.m, G::BM, G::kAByK) + in_row;
-  int64_t col = G::origin(tn * G::kCols, g.n, G::kCols, G::kBByK) + in_col;
+  const int64_t row = G::origin(tm * G::BM, g.m, G::BM) + in_row;
+  int64_t col = G::origin(tn * G::kCols, g.n, G::kCols) + in_col;
   const int over = (int)(tn * G::kCols - col);
   if (row >= g.m || row < tm * G::BM || col >= g.n || over >= 8) return;
   float v[8] = {}, u[8] = {};

@@ -30,7 +30,7 @@ hipError_t launch_product(const GemmPlan& p, GemmArgs g, hipStream_t stream) {
     return launch_with<Gemm<DT, LA, LB, 64, 64, 2, 2, 1, EPI, false>>(p, g, stream);
   }
   if constexpr (DT != kFP32) {
-    if (p.tile == kTileL) return launch_with<Gemm<DT, LA, LB, 256, 256, 2, 4, 1, EPI, true>>(p, g, stream);
+    if (p.tile == kTileL) return launch_with<Gemm<DT, LA, LB, 256, 256, 2, 2, 1, EPI, true>>(p, g, stream);
   }
   return launch_with<Gemm<DT, LA, LB, 128, 128, 2, 2, 1, EPI, true>>(p, g, stream);
 }

@@ -5,7 +5,7 @@
 namespace triaccel {
 namespace layers {
 
-// S: 64 x 64, staged.  M: 128 x 128, L: 256 x 256, both straight to LDS.
+// S: 64 x 64, staged.  M: 128 x 128, L: 256 x 256, both in the wide form.
 enum Tile : int { kTileS = 0, kTileM = 1, kTileL = 2 };
 
 struct GemmPlan {
@@ -30,10 +30,10 @@ inline GemmPlan plan_tile(int tile, bool fp32, bool gated, int64_t m, int64_t n,
   const int64_t k_tiles = seg > 0 ? ceil_div(seg, bk) * nseg : 1, all = (int64_t)p.tiles_m * p.tiles_n;
   p.groups = tile == kTileS && k_tiles >= 4 && all <= 512 ? (fp32 ? 2 : 4) : 1;
   // microseconds of a tile of k, and of what a workgroup has besides
-  const double per_k = tile == kTileL ? 0.95 : tile == kTileM ? (fp32 ? 1.3 : 0.75) : (fp32 ? 1.6 : 1.0) / p.groups, fixed = 5.0;
+  const double per_k = tile == kTileL ? 0.9 : tile == kTileM ? (fp32 ? 1.3 : 0.75) : (fp32 ? 2.7 : 1.0) / p.groups, fixed = 5.0;
   const int64_t slots = tile == kTileL ? 256 : tile == kTileM ? (fp32 ? 256 : 512) : p.groups > 1 ? 256 : 1024;
   const int64_t rounds = all / slots, rest = all % slots;
-  const int64_t least = tile == kTileS ? 4 * p.groups : 4;  // tiles of k that a share has at least
+  const int64_t least = tile == kTileS ? 4 * p.groups : 8;  // tiles of k that a share has at least
   p.whole = (int32_t)all;
   p.splits = 1;
   p.per_split = (int32_t)k_tiles;
@@ -59,13 +59,13 @@ inline GemmPlan plan_tile(int tile, bool fp32, bool gated, int64_t m, int64_t n,
 }
 
 // m x n results (gated: n columns of two products), k = nseg segments of seg.  `pack_us`: what it takes to lay the operands out
-// for the direct form.
+// for the wide form.
 inline GemmPlan plan_gemm(bool fp32, bool gated, double pack_us, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
   GemmPlan best = plan_tile(kTileS, fp32, gated, m, n, seg, nseg);
   for (int tile = kTileM; tile <= (fp32 ? kTileM : kTileL); ++tile) {
     const int64_t edge = tile == kTileL ? 256 : 128;
-    // the direct form shifts its last tiles inwards: the result is no smaller than one of them
-    if (m < edge || n * (gated ? 2 : 1) < edge || seg < 1) continue;
+    // the wide form shifts its last tiles inwards: the result is no smaller than one of them, nor k than a unit
+    if (m < edge || n * (gated ? 2 : 1) < edge || seg < 8) continue;
     const GemmPlan p = plan_tile(tile, fp32, gated, m, n, seg, nseg);
     if (p.us + pack_us < best.us + (best.tile == kTileS ? 0.0 : pack_us)) best = p;
   }

@@ -96,20 +96,14 @@ hipError_t run_product(int32_t dtype, Product kind, const GemmPlan& p, const Gem
          : dtype == TRIACCEL_BF16 ? launch_gemm_bf16(kind, p, g, s) : launch_gemm_fp32(kind, p, g, s);
 }
 
-// An operand as the caller (or the workspace) has it.  `room`: its rows may be read up to a whole unit of eight, zeros.
+// An operand as the caller (or the workspace) has it.
 struct Operand {
   const void* p;
   int64_t ld, rows, cols;
-  bool room;
 };
-// Whether its 16-byte units can go straight to LDS as they lie: whole, aligned, a tile's rows within 31 bits of its first.
-bool as_it_lies(int32_t dtype, const Operand& o) {
-  return dtype != TRIACCEL_FP32 && (o.room || o.cols % 8 == 0) && (reinterpret_cast<uintptr_t>(o.p) & 15u) == 0 && o.ld % 8 == 0 && o.ld < (1 << 21);
-}
+// Only fp32 is laid out anew, in its three parts.
 int64_t packed_ld(const Operand& o) { return (o.cols + 7) / 8 * 8; }
-uint64_t packed_bytes(int32_t dtype, const Operand& o) {
-  return padded((uint64_t)o.rows * (uint64_t)packed_ld(o) * (dtype == TRIACCEL_FP32 ? 6u : 2u));
-}
+uint64_t packed_bytes(const Operand& o) { return padded((uint64_t)o.rows * (uint64_t)packed_ld(o) * 6u); }
 
 // Up to three operands (the second matrix of a gated block among them) and up to two products of them, planned together:
 // what is laid out anew is laid out once.
@@ -121,32 +115,27 @@ struct Products {
   uint64_t at[4];      // in the workspace
   uint64_t partial, total;
 };
-// The two weights of a gated block are read with one stride: both as they lie, or both anew.
-bool in_place(const Products& q, int i) {
-  if (i == 1 || i == 2) return as_it_lies(q.dtype, q.op[1]) && (!q.op[2].rows || as_it_lies(q.dtype, q.op[2]));
-  return as_it_lies(q.dtype, q.op[i]);
-}
-// `need`: bit i = a direct product reads operand i.
+// `need`: bit i = a product in the wide form reads operand i.
 void lay_out(Products& q, uint64_t from, unsigned need, uint64_t partial_bytes) {
   uint64_t at = from;
   for (int i = 0; i < 4; ++i) {
-    q.pack[i] = (need >> i & 1u) && q.op[i].rows > 0 && !in_place(q, i);
+    q.pack[i] = q.dtype == TRIACCEL_FP32 && (need >> i & 1u) && q.op[i].rows > 0;
     q.at[i] = at;
-    if (q.pack[i]) at += packed_bytes(q.dtype, q.op[i]);
+    if (q.pack[i]) at += packed_bytes(q.op[i]);
   }
   q.partial = at;
   q.total = at + padded(partial_bytes);
 }
-// What laying out the operands in `need` costs, in the plan's microseconds; more than anything where it cannot be done.
+// What laying out the operands in `need` costs, in the plan's microseconds; more than anything where the wide form cannot be
+// used: a tile's rows have to lie within 31 bits, and one launch lays everything out.
 double pack_us(const Products& q, unsigned need) {
   uint64_t bytes = 0;
   for (int i = 0; i < 4; ++i) {
     if (!(need >> i & 1u)) continue;
-    // a tile's rows lie within 31 bits, and one launch lays everything out
-    if (q.op[i].cols >= (1 << 21) || q.op[i].rows * q.op[i].cols >= (int64_t)1 << 32) return 1e30;
-    if (!in_place(q, i)) bytes += 2 * packed_bytes(q.dtype, q.op[i]);
+    if (q.op[i].cols >= (1 << 21) || q.op[i].ld >= (1 << 21) || q.op[i].rows * q.op[i].cols >= (int64_t)1 << 32) return 1e30;
+    bytes += packed_bytes(q.op[i]) / 6 * 10;
   }
-  return bytes ? 6.0 + (double)bytes / 4.0e6 : 0.0;
+  return q.dtype == TRIACCEL_FP32 && bytes ? 6.0 + (double)bytes / 4.0e6 : 0.0;
 }
 int pack(const Products& q, char* ws, hipStream_t s) {
   PackArgs a{};
@@ -173,9 +162,9 @@ ForwardPlan plan_forward(int32_t dtype, Product kind, int64_t rows, int64_t in, 
   ForwardPlan f{};
   f.q.dtype = dtype;
   const bool two = kind == kGatedForward;
-  f.q.op[1] = Operand{w, ldw, out, in, false};
-  if (two) f.q.op[2] = Operand{w2, ldw, out, in, false};
-  f.q.op[3] = Operand{x, ldx, rows, in, false};
+  f.q.op[1] = Operand{w, ldw, out, in};
+  if (two) f.q.op[2] = Operand{w2, ldw, out, in};
+  f.q.op[3] = Operand{x, ldx, rows, in};
   unsigned need = two ? 14u : 10u;
   f.g = plan_gemm(dtype == TRIACCEL_FP32, two, pack_us(f.q, need), rows, out, in, 1);
   if (f.g.tile == kTileS) need = 0;
@@ -211,10 +200,10 @@ BackwardPlan plan_backward(const BackwardShape& b, const void* ws) {
   const uint64_t from = l.sums + (b.sums ? padded((uint64_t)l.blocks * (uint64_t)(b.wide * b.out) * 4u) : 0);
   Products& q = l.q;
   q.dtype = b.dtype;
-  q.op[0] = b.slope ? Operand{ws, b.wide * l.width, b.rows, b.wide * l.width, true} : Operand{b.dy, b.lddy, b.rows, b.out, false};
-  q.op[1] = Operand{b.w, b.ldw, b.out, b.in, false};
-  if (b.wide == 2) q.op[2] = Operand{b.w2, b.ldw, b.out, b.in, false};
-  q.op[3] = Operand{b.x, b.ldx, b.rows, b.in, false};
+  q.op[0] = b.slope ? Operand{ws, b.wide * l.width, b.rows, b.wide * l.width} : Operand{b.dy, b.lddy, b.rows, b.out};
+  q.op[1] = Operand{b.w, b.ldw, b.out, b.in};
+  if (b.wide == 2) q.op[2] = Operand{b.w2, b.ldw, b.out, b.in};
+  q.op[3] = Operand{b.x, b.ldx, b.rows, b.in};
   const bool fp32 = b.dtype == TRIACCEL_FP32;
   unsigned need_dx = b.wide == 2 ? 7u : 3u, need_dw = 9u, need = 0;
   uint64_t partial = 0;
