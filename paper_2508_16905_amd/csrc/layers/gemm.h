@@ -461,22 +461,24 @@ struct Gemm {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   }
-  // The order in which a stage's instructions are issued: reads of LDS first, then what goes to it and the loads that take its
-  // place in the registers, each behind some products, so that the matrix cores have work meanwhile.  Left alone the compiler
-  // puts all reads first and all products last.
-  template <int READS, int WRITES, int MFMA>
+  // The order in which a stage's instructions are issued: reads of LDS first, then what goes to it and the loads, each behind
+  // some products, so that the matrix cores have work meanwhile.  Left alone the compiler puts all reads first and all
+  // products last.  The loads are spread over both stages of a tile (8192 x 10240 -> 4096 in bf16: 675 us with all of them
+  // in the first, 719 in the second, 646 in both).
+  template <int READS, int WRITES, int LOADS, int MFMA>
   static __device__ __forceinline__ void interleave() {
-    constexpr int kEach = MFMA / (READS + 2 * WRITES + 1) > 0 ? MFMA / (READS + 2 * WRITES + 1) : 1;
+    constexpr int kTail = WRITES > LOADS ? WRITES : LOADS;
+    constexpr int kEach = MFMA / (READS + 2 * kTail + 1) > 0 ? MFMA / (READS + 2 * kTail + 1) : 1;
 #pragma unroll
     for (int i = 0; i < READS; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
 #pragma unroll
-    for (int i = 0; i < WRITES; ++i) {
+    for (int i = 0; i < kTail; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
-      __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      if (i < WRITES) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+      if (i < LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x008, MFMA, 0);
@@ -515,23 +517,30 @@ struct Gemm {
         for (int t = 0; t < TB; ++t) put<LB, BN>(to + kPlanes * BM * BK, t, q, in_place<LB, BN>(g, w, rb[t][q], t, id), id);
       }
     };
-    // tile kt + 1 from the registers to LDS, tile kt + 2, a whole one, into them
-    const auto pass_on = [&](int kt) {
-      const At w = at(g, kt + 2);
-      short* to = buffer(kt + 1);
+    // the same for a whole tile, in the loop
+    const auto store_whole = [&](int kt) {
+      short* to = buffer(kt);
 #pragma unroll
       for (int q = 0; q < kPlanes; ++q) {
 #pragma unroll
-        for (int t = 0; t < TA; ++t) {
-          put<LA, BM>(to, t, q, ra[t][q], tid);
-          ra[t][q] = get<LA, BM, false>(g, w, r0, t, q, off_a, wave);
-        }
+        for (int t = 0; t < TA; ++t) put<LA, BM>(to, t, q, ra[t][q], tid);
 #pragma unroll
-        for (int t = 0; t < TB; ++t) {
-          put<LB, BN>(to + kPlanes * BM * BK, t, q, rb[t][q], tid);
-          rb[t][q] = get<LB, BN, true>(g, w, c0, t, q, off_b, wave);
-        }
+        for (int t = 0; t < TB; ++t) put<LB, BN>(to + kPlanes * BM * BK, t, q, rb[t][q], tid);
       }
+    };
+    const auto load_a = [&](int kt) {
+      const At w = at(g, kt);
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q)
+#pragma unroll
+        for (int t = 0; t < TA; ++t) ra[t][q] = get<LA, BM, false>(g, w, r0, t, q, off_a, wave);
+    };
+    const auto load_b = [&](int kt) {
+      const At w = at(g, kt);
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q)
+#pragma unroll
+        for (int t = 0; t < TB; ++t) rb[t][q] = get<LB, BN, true>(g, w, c0, t, q, off_b, wave);
     };
     constexpr int kMfma = (kPlanes == 3 ? 6 : 1) * FM * FN, kWrites = kPlanes * (TA + TB);
     constexpr int kReads = kPlanes * (FM * (LA == KS ? 2 : 1) + FN * (LB == KS ? 2 : 1));
@@ -547,25 +556,29 @@ struct Gemm {
         if constexpr (BK == 64) {
           do {
             read(f1, buffer(kt), 32, wm, wn, lane);
-            pass_on(kt);
+            store_whole(kt + 1);
+            load_a(kt + 2);
             multiply<0, FM>(acc, f0);
-            interleave<kReads, kWrites, kMfma>();
+            interleave<kReads, kWrites, kPlanes * TA, kMfma>();
             meet();
             read(f0, buffer(kt + 1), 0, wm, wn, lane);
+            load_b(kt + 2);
             multiply<0, FM>(acc, f1);
-            interleave<kReads, 0, kMfma>();
+            interleave<kReads, 0, kPlanes * TB, kMfma>();
             __builtin_amdgcn_sched_barrier(0);
             ++kt;
           } while (whole(kt + 2));
         } else {
           const auto turn = [&](Frags& now, Frags& next) {
-            pass_on(kt);
+            store_whole(kt + 1);
+            load_a(kt + 2);
             multiply<0, FM / 2>(acc, now);
-            interleave<0, kWrites, kMfma / 2>();
+            interleave<0, kWrites, kPlanes * TA, kMfma / 2>();
             meet();
             read(next, buffer(kt + 1), 0, wm, wn, lane);
+            load_b(kt + 2);
             multiply<FM / 2, FM>(acc, now);
-            interleave<kReads, 0, kMfma / 2>();
+            interleave<kReads, 0, kPlanes * TB, kMfma / 2>();
             __builtin_amdgcn_sched_barrier(0);
             ++kt;
           };

@@ -30,7 +30,7 @@ inline GemmPlan plan_tile(int tile, bool fp32, bool gated, int64_t m, int64_t n,
   const int64_t k_tiles = seg > 0 ? ceil_div(seg, bk) * nseg : 1, all = (int64_t)p.tiles_m * p.tiles_n;
   p.groups = tile == kTileS && k_tiles >= 4 && all <= 512 ? (fp32 ? 2 : 4) : 1;
   // microseconds of a tile of k, and of what a workgroup has besides
-  const double per_k = tile == kTileL ? 0.9 : tile == kTileM ? (fp32 ? 1.3 : 0.75) : (fp32 ? 2.7 : 1.0) / p.groups, fixed = 5.0;
+  const double per_k = tile == kTileL ? 1.75 : tile == kTileM ? (fp32 ? 1.85 : all > 256 ? 1.45 : 1.0) : (fp32 ? 2.7 : 1.2) / p.groups, fixed = 5.0;
   const int64_t slots = tile == kTileL ? 256 : tile == kTileM ? (fp32 ? 256 : 512) : p.groups > 1 ? 256 : 1024;
   const int64_t rounds = all / slots, rest = all % slots;
   const int64_t least = tile == kTileS ? 4 * p.groups : 8;  // tiles of k that a share has at least
