@@ -11,9 +11,10 @@
 // products the six largest are summed, those of one scale in one accumulator; what is dropped is at most 2^-26 of a product.
 // Six bf16 products have 2.6 times the rate of the fp32 matrix instructions (2.5 PFLOP/s / 6 = 417 and 157 TFLOP/s).
 //
-// Two forms.  WIDE: a tile ahead in registers, fragments of the next 32 k ahead of these products, any strides and alignment
-// (fp32: the operands' parts, laid out by k_pack); the result has the size of a tile at least.  Staged: small tiles, any
-// sizes, with fp32 split on the way; for small products, where KG groups of wavefronts share the k of one tile.
+// Three forms.  Wide: a tile ahead in registers, fragments of the next 32 k ahead of these products, any strides and alignment
+// (fp32: the operands' parts, laid out by k_pack); the result has the size of a tile at least.  Staged: small tiles,
+// fp32 split on the way; for small products, where KG groups of wavefronts share the k of one tile; no operand's rows are
+// shorter than eight.  Short: the same with operands loaded element by element, for those that have shorter rows.
 #pragma once
 #include <type_traits>
 
@@ -23,6 +24,7 @@ namespace triaccel {
 namespace layers {
 
 enum Layout : int { KC = 0, KS = 1 };
+enum Form : int { kStaged = 0, kWide = 1, kShort = 2 };
 enum Epi : int { kEpiLinear = 0, kEpiGated = 1, kEpiStore = 2 };
 
 struct GemmArgs {
@@ -125,15 +127,15 @@ __device__ __forceinline__ void epi_row(const GemmArgs& g, const ColumnState& s,
 // that eight rows' reads of one k fall on all banks.  KS: k after k of R rows, pairs of units exchanged by k: an instruction
 // that turns reads 32 bytes of each of sixteen k.
 template <int L, int R, int BK>
-__device__ __forceinline__ int tile_unit(int row_or_k, int unit) {
+__device__ __forceinline__ uint32_t tile_unit(uint32_t row_or_k, uint32_t unit) {
   if constexpr (L == KC) {
     constexpr int kUnits = BK / 8;
-    const int x = kUnits >= 8 ? (row_or_k & 7) : ((row_or_k >> 1) & (kUnits - 1));
+    const uint32_t x = kUnits >= 8 ? (row_or_k & 7) : ((row_or_k >> 1) & (kUnits - 1));
     return row_or_k * kUnits + (unit ^ x);
   } else {
     constexpr int kUnits = R / 8;
-    const int f = (row_or_k & 3) | ((row_or_k >> 1) & 4);
-    const int x = (f & (kUnits / 2 - 1)) << 1;
+    const uint32_t f = (row_or_k & 3) | ((row_or_k >> 1) & 4);
+    const uint32_t x = (f & (kUnits / 2 - 1)) << 1;
     return row_or_k * kUnits + (unit ^ x);
   }
 }
@@ -174,8 +176,9 @@ __device__ __forceinline__ int on_xcd(int id, int total) {
   return xcd * per + (xcd < more ? xcd : more) + (id >> 3);
 }
 
-template <int DT_, int LA, int LB, int BM_, int BN_, int WR, int WC, int KG, int EPI_, bool WIDE>
+template <int DT_, int LA, int LB, int BM_, int BN_, int WR, int WC, int KG, int EPI_, int FORM>
 struct Gemm {
+  static constexpr bool WIDE = FORM == kWide;
   static constexpr int DT = DT_, BM = BM_, BN = BN_, EPI = EPI_;
   static constexpr int kPlanes = DT == kFP32 ? 3 : 1;
   static constexpr int BK = DT == kFP32 ? 32 : 64;
@@ -199,7 +202,7 @@ struct Gemm {
   typedef typename std::conditional<WIDE, __bf16, Elem<DT>>::type E;  // WIDE: any 16 bits
   typedef f32x4 Acc[kPlanes][FM][FN];  // [q]: what counts 2^-8q
 
-  // Where the tile of the result begins whose first row is `r0`, and likewise for columns.  WIDE: the last tile begins
+  // Where the tile of the result begins whose first row is `r0`, and likewise for columns.  Wide: the last tile begins
   // earlier, so that it lies inside (the plan has m >= BM and n >= kCols); what the one before it has is not stored twice.
   static __device__ __forceinline__ int origin(int r0, int rows, int size) {
     if (!WIDE) return r0;
@@ -302,47 +305,93 @@ struct Gemm {
     }
   }
   template <int L, int R>
-  static __device__ __forceinline__ void put(short* tile, int t, int q, s16x8 v, int tid) {
-    const int slot = t * NT + tid;
-    const int u = L == KC ? tile_unit<KC, R, BK>(slot / (BK / 8), slot % (BK / 8)) : tile_unit<KS, R, BK>(slot / (R / 8), slot % (R / 8));
+  static __device__ __forceinline__ void put(short* tile, int t, int q, s16x8 v, uint32_t tid) {
+    const uint32_t slot = t * NT + tid;
+    const uint32_t u = L == KC ? tile_unit<KC, R, BK>(slot / (BK / 8), slot % (BK / 8)) : tile_unit<KS, R, BK>(slot / (R / 8), slot % (R / 8));
     *(s16x8*)(tile + q * R * BK + 8 * u) = v;
   }
 
-  // --- through registers ---
+  // --- staged form ---
+  // Loads without a branch per lane: a unit that would pass the end of its row (of k, or of the result's rows) is loaded from
+  // eight before that end, and a row past the last one is the last one; once they have arrived (`settle`) units are moved to
+  // their place, zeros behind.
+  // How far (bytes) unit t NT + tid lies from the tile's beginning in k; the same for all tiles.
   template <int L, int R, int T, bool IS_B>
-  static __device__ __forceinline__ void fetch(const GemmArgs& g, const At& w, int r0, int rows, Elem8<DT> (&out)[T], int tid) {
+  static __device__ __forceinline__ void offsets(const GemmArgs& g, int r0, int rows, int64_t (&off)[T], uint32_t tid) {
     const int64_t ld = IS_B ? g.ldb : g.lda;
-    const int64_t seg0 = IS_B ? 0 : (int64_t)w.seg * g.seg_step;
-    const E* p0 = (const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a);
-    const bool inside = w.left >= BK && (L == KC || r0 + R <= rows);
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      const int slot = t * NT + tid;
+      const uint32_t slot = t * NT + tid;
       if constexpr (L == KC) {
-        const int row = slot / (BK / 8), unit = slot % (BK / 8);
         bool second = false;
-        int r = r0 + (IS_B ? b_row(row, second) : row);
-        r = r < rows ? r : rows - 1;  // a row of the result that is not written
-        const E* q = (second ? (const E*)g.b2 : p0) + (int64_t)r * ld + seg0;
-        out[t] = inside ? load_raw8<DT>(q + w.k0 + unit * 8) : load_edge8<DT>(q, w.k0 + unit * 8, g.seg);
+        int r = r0 + (IS_B ? b_row((int)(slot / (BK / 8)), second) : (int)(slot / (BK / 8)));
+        r = r < rows ? r : rows - 1;
+        off[t] = ((int64_t)r * ld + slot % (BK / 8) * 8) * (int64_t)sizeof(E);
       } else {
-        const int k = slot / (R / 8), c = r0 + slot % (R / 8) * 8;
-        const E* q = p0 + (seg0 + w.k0 + (k < w.left ? k : w.left - 1)) * ld;
-        if (inside) {
-          out[t] = load_raw8<DT>(q + c);
-        } else {
-          out[t] = load_edge8<DT>(q, c, rows);
-          if (k >= w.left) out[t] = Elem8<DT>{};
-        }
+        const int at = r0 + (int)(slot % (R / 8) * 8), last = rows >= 8 ? rows - 8 : 0;
+        off[t] = ((int64_t)(slot / (R / 8)) * ld + (at < last ? at : last)) * (int64_t)sizeof(E);
       }
     }
   }
-  template <int L, int R, int T>
-  static __device__ __forceinline__ void place(const Elem8<DT> (&in)[T], short* tile, int tid) {
+  template <int L, int R, int T, bool IS_B>
+  static __device__ __forceinline__ void fetch(const GemmArgs& g, const At& w, int rows, const int64_t (&off)[T], Elem8<DT> (&out)[T], uint32_t tid) {
+    const int64_t ld = IS_B ? g.ldb : g.lda;
+    const int64_t k0 = (IS_B ? 0 : w.seg * (int64_t)g.seg_step) + w.k0;
+    const char* base = (const char*)((const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a) + (L == KC ? k0 : k0 * ld));
+    const char* base2 = (const char*)((const E*)g.b2 + k0);
+    const int len = L == KC ? g.seg : rows;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      const int slot = t * NT + tid;
-      const int u = L == KC ? tile_unit<KC, R, BK>(slot / (BK / 8), slot % (BK / 8)) : tile_unit<KS, R, BK>(slot / (R / 8), slot % (R / 8));
+      const uint32_t slot = t * NT + tid;
+      const char* from = base;
+      if constexpr (EPI == kEpiGated && IS_B && L == KC) {  // a wavefront's rows are all of one matrix
+        bool second;
+        b_row((int)((uint32_t)__builtin_amdgcn_readfirstlane((int)slot) / (BK / 8)), second);
+        if (second) from = base2;
+      }
+      int64_t at = off[t];
+      if (w.left < BK) {
+        if constexpr (L == KC) {
+          const int past = (int)(slot % (BK / 8) * 8) - (w.left - 8);
+          at -= (past > 0 ? (int64_t)past : 0) * (int64_t)sizeof(E);
+        } else {
+          const int past = (int)(slot / (R / 8)) - (w.left - 1);
+          at -= (past > 0 ? past * ld : 0) * (int64_t)sizeof(E);
+        }
+      }
+      const E* p = (const E*)(from + at);
+      if constexpr (FORM == kStaged) {
+        out[t] = load_raw8<DT>(p);
+      } else {  // rows may be shorter than a unit: those from their beginning, element by element
+        if (L == KC && len < 8) p += 8 - w.left;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) out[t][i] = *as_global<E>(p + (i < len ? i : len - 1));
+      }
+    }
+  }
+  template <int L, int R, int T, bool IS_B>
+  static __device__ __forceinline__ void settle(const GemmArgs& g, const At& w, int r0, int rows, Elem8<DT> (&v)[T], uint32_t tid) {
+    const int len = L == KC ? g.seg : rows;
+    if (L == KC ? w.left >= BK : w.left >= BK && r0 + R <= rows) return;
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const uint32_t slot = t * NT + tid;
+      const int at = L == KC ? w.k0 + (int)(slot % (BK / 8) * 8) : r0 + (int)(slot % (R / 8) * 8);
+      const int past = FORM == kStaged || len >= 8 ? at - (len - 8) : at;  // how far to move; a short row was loaded from its beginning
+      move_units<DT>(v[t], past > 0 ? past : 0);
+      if (FORM == kShort && len < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[t][i] = at + i < len ? v[t][i] : (E)0.0f;
+      }
+      if (L == KS && (int)(slot / (R / 8)) >= w.left) v[t] = Elem8<DT>{};
+    }
+  }
+  template <int L, int R, int T>
+  static __device__ __forceinline__ void place(const Elem8<DT> (&in)[T], short* tile, uint32_t tid) {
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+      const uint32_t slot = t * NT + tid;
+      const uint32_t u = L == KC ? tile_unit<KC, R, BK>(slot / (BK / 8), slot % (BK / 8)) : tile_unit<KS, R, BK>(slot / (R / 8), slot % (R / 8));
       if constexpr (DT == kFP32) {
         s16x8 part[3];
         split3(in[t], part);
@@ -602,37 +651,51 @@ struct Gemm {
     }
   }
 
-  // Group kg of KG has tiles first + kg, first + kg + KG, ...
+  // Group kg of KG has tiles first + kg, first + kg + KG, ...  What such a product waits for is memory, a round trip per tile:
+  // kAhead tiles of a group are on their way to its registers.
+  static constexpr int kAhead = 3;
   static __device__ __forceinline__ void staged_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int kg, int tid, int wm, int wn, int lane) {
-    Elem8<DT> ra[TA], rb[TB];
-    const auto load = [&](int kt) {
+    Elem8<DT> ra[kAhead][TA], rb[kAhead][TB];
+    int64_t off_a[TA], off_b[TB];
+    offsets<LA, BM, TA, false>(g, r0, g.m, off_a, tid);
+    offsets<LB, BN, TB, true>(g, c0, g.n, off_b, tid);
+    const auto load = [&](int kt, int set) {
       const At w = at(g, kt);
-      fetch<LA, BM, TA, false>(g, w, r0, g.m, ra, tid);
-      fetch<LB, BN, TB, true>(g, w, c0, g.n, rb, tid);
-    };
-    const auto put_all = [&](short* to) {
-      place<LA, BM, TA>(ra, to, tid);
-      place<LB, BN, TB>(rb, to + kPlanes * BM * BK, tid);
+      fetch<LA, BM, TA, false>(g, w, g.m, off_a, ra[set], tid);
+      fetch<LB, BN, TB, true>(g, w, g.n, off_b, rb[set], tid);
     };
     short* mine = lds + kg * 2 * kTile;
-    if (first + kg < last) {
-      load(first + kg);
-      put_all(mine);
-    }
-    int at = 0;
-    for (int kt = first; kt < last; kt += KG, at ^= 1) {
-      __syncthreads();
-      const int now = kt + kg, next = now + KG;
-      if (next < last) load(next);
-      if (now < last) {
+    int now = first + kg, buf = 0;
 #pragma unroll
-        for (int k0 = 0; k0 < BK; k0 += 32) {
-          Frags f;
-          read(f, mine + at * kTile, k0, wm, wn, lane);
-          multiply<0, FM>(acc, f);
+    for (int i = 0; i < kAhead; ++i)
+      if (now + i * KG < last) load(now + i * KG, i);
+    // all groups take as many turns as the first
+    for (int turn = first; turn < last;) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (turn >= last) break;
+        short* to = mine + buf * kTile;
+        if (now < last) {
+          const At w = at(g, now);
+          settle<LA, BM, TA, false>(g, w, r0, g.m, ra[i], tid);
+          settle<LB, BN, TB, true>(g, w, c0, g.n, rb[i], tid);
+          place<LA, BM, TA>(ra[i], to, tid);
+          place<LB, BN, TB>(rb[i], to + kPlanes * BM * BK, tid);
         }
+        meet();
+        if (now + kAhead * KG < last) load(now + kAhead * KG, i);
+        if (now < last) {
+#pragma unroll
+          for (int k0 = 0; k0 < BK; k0 += 32) {
+            Frags f;
+            read(f, to, k0, wm, wn, lane);
+            multiply<0, FM>(acc, f);
+          }
+        }
+        buf ^= 1;
+        now += KG;
+        turn += KG;
       }
-      if (next < last) put_all(mine + (at ^ 1) * kTile);
     }
   }
 

@@ -3,6 +3,7 @@
 #include "gemm.h"
 #include "gemm_plan.h"
 #include "layers.h"
+#include "thin.h"
 
 namespace triaccel {
 namespace layers {
@@ -25,18 +26,29 @@ hipError_t launch_product(const GemmPlan& p, GemmArgs g, hipStream_t stream) {
   g.splits = p.splits;
   g.per_split = p.per_split;
   constexpr int kGroups = DT == kFP32 ? 2 : 4;
+  if (p.tile == kTileShort) return launch_with<Gemm<DT, LA, LB, 64, 64, 2, 2, 1, EPI, kShort>>(p, g, stream);
   if (p.tile == kTileS) {
-    if (p.groups > 1) return launch_with<Gemm<DT, LA, LB, 64, 64, 2, 2, kGroups, EPI, false>>(p, g, stream);
-    return launch_with<Gemm<DT, LA, LB, 64, 64, 2, 2, 1, EPI, false>>(p, g, stream);
+    if (p.groups > 1) return launch_with<Gemm<DT, LA, LB, 64, 64, 2, 2, kGroups, EPI, kStaged>>(p, g, stream);
+    return launch_with<Gemm<DT, LA, LB, 64, 64, 2, 2, 1, EPI, kStaged>>(p, g, stream);
   }
   if constexpr (DT != kFP32) {
-    if (p.tile == kTileL) return launch_with<Gemm<DT, LA, LB, 256, 256, 2, 2, 1, EPI, true>>(p, g, stream);
+    if (p.tile == kTileL) return launch_with<Gemm<DT, LA, LB, 256, 256, 2, 2, 1, EPI, kWide>>(p, g, stream);
   }
-  return launch_with<Gemm<DT, LA, LB, 128, 128, 2, 2, 1, EPI, true>>(p, g, stream);
+  return launch_with<Gemm<DT, LA, LB, 128, 128, 2, 2, 1, EPI, kWide>>(p, g, stream);
+}
+
+template <int DT, int EPI>
+hipError_t launch_thin(const GemmArgs& g, hipStream_t stream) {
+  // a wavefront has two steps of 32 k at least, so that short k do not pay for sixteen wavefronts
+  int waves = (g.seg + 63) / 64;
+  waves = waves < 1 ? 1 : waves > kThinWaves ? kThinWaves : waves;
+  k_thin<DT, EPI><<<dim3((uint32_t)ceil_div(g.n, kThinCols)), waves * 64, 0, stream>>>(g);
+  return hipGetLastError();
 }
 
 template <int DT>
 hipError_t launch_any(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream) {
+  if (p.tile == kTileThin) return kind == kForward ? launch_thin<DT, kEpiLinear>(g, stream) : launch_thin<DT, kEpiGated>(g, stream);
   switch (kind) {
     case kForward: return launch_product<DT, KC, KC, kEpiLinear>(p, g, stream);
     case kGatedForward: return launch_product<DT, KC, KC, kEpiGated>(p, g, stream);

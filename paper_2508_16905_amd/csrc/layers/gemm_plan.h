@@ -6,7 +6,8 @@ namespace triaccel {
 namespace layers {
 
 // S: 64 x 64, staged.  M: 128 x 128, L: 256 x 256, both in the wide form.
-enum Tile : int { kTileS = 0, kTileM = 1, kTileL = 2 };
+// Short: as S, where an operand's rows are shorter than eight.  Thin: forward products of at most 16 rows (thin.h).
+enum Tile : int { kTileS = 0, kTileM = 1, kTileL = 2, kTileShort = 3, kTileThin = 4 };
 
 struct GemmPlan {
   int tile, groups;         // groups: of wavefronts that share the k of a tile (S)
@@ -28,12 +29,13 @@ inline GemmPlan plan_tile(int tile, bool fp32, bool gated, int64_t m, int64_t n,
   p.tiles_m = (int32_t)ceil_div(m, edge);
   p.tiles_n = (int32_t)ceil_div(n * half, edge);
   const int64_t k_tiles = seg > 0 ? ceil_div(seg, bk) * nseg : 1, all = (int64_t)p.tiles_m * p.tiles_n;
+  const bool small = tile == kTileS || tile == kTileShort;
   p.groups = tile == kTileS && k_tiles >= 4 && all <= 512 ? (fp32 ? 2 : 4) : 1;
   // microseconds of a tile of k, and of what a workgroup has besides
   const double per_k = tile == kTileL ? 1.75 : tile == kTileM ? (fp32 ? 1.85 : all > 256 ? 1.45 : 1.0) : (fp32 ? 2.7 : 1.2) / p.groups, fixed = 5.0;
   const int64_t slots = tile == kTileL ? 256 : tile == kTileM ? (fp32 ? 256 : 512) : p.groups > 1 ? 256 : 1024;
   const int64_t rounds = all / slots, rest = all % slots;
-  const int64_t least = tile == kTileS ? 4 * p.groups : 8;  // tiles of k that a share has at least
+  const int64_t least = small ? 4 * p.groups : 8;  // tiles of k that a share has at least
   p.whole = (int32_t)all;
   p.splits = 1;
   p.per_split = (int32_t)k_tiles;
@@ -60,7 +62,9 @@ inline GemmPlan plan_tile(int tile, bool fp32, bool gated, int64_t m, int64_t n,
 
 // m x n results (gated: n columns of two products), k = nseg segments of seg.  `pack_us`: what it takes to lay the operands out
 // for the wide form.
-inline GemmPlan plan_gemm(bool fp32, bool gated, double pack_us, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
+// `shortest`: the shortest row of an operand.
+inline GemmPlan plan_gemm(bool fp32, bool gated, double pack_us, int64_t shortest, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
+  if (shortest < 8) return plan_tile(kTileShort, fp32, gated, m, n, seg, nseg);
   GemmPlan best = plan_tile(kTileS, fp32, gated, m, n, seg, nseg);
   for (int tile = kTileM; tile <= (fp32 ? kTileM : kTileL); ++tile) {
     const int64_t edge = tile == kTileL ? 256 : 128;

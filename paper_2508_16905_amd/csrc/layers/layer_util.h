@@ -51,30 +51,34 @@ __device__ __forceinline__ void move_down(uint32_t (&w)[4], int halves) {
     w[i] = halves == 8 ? 0u : w[i];
   }
 }
+// v[s], v[s + 1], ... to the front, zeros behind (s >= 8: zeros).
+template <int DT>
+__device__ __forceinline__ void move_units(Elem8<DT>& v, int s) {
+  if constexpr (DT == kFP32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = s & 4 ? (i < 4 ? v[(i + 4) & 7] : 0.0f) : v[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = s & 2 ? (i < 6 ? v[(i + 2) & 7] : 0.0f) : v[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = s & 1 ? (i < 7 ? v[(i + 1) & 7] : 0.0f) : v[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = s >= 8 ? 0.0f : v[i];
+  } else {
+    typedef __attribute__((ext_vector_type(4))) uint32_t W;
+    W x = __builtin_bit_cast(W, v);
+    uint32_t w[4] = {x[0], x[1], x[2], x[3]};
+    move_down(w, s);
+    x = W{w[0], w[1], w[2], w[3]};
+    v = __builtin_bit_cast(Elem8<DT>, x);
+  }
+}
 template <int DT>
 __device__ __forceinline__ Elem8<DT> load_edge8(const Elem<DT>* row, int64_t at, int64_t len) {
   Elem8<DT> v;
   if (len >= 8) {
     const int64_t from = at < len - 8 ? at : len - 8;
-    const int s = at - from < 8 ? (int)(at - from) : 8;
     v = load_raw8<DT>(row + from);
-    if constexpr (DT == kFP32) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = s & 4 ? (i < 4 ? v[i + 4 & 7] : 0.0f) : v[i];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = s & 2 ? (i < 6 ? v[i + 2 & 7] : 0.0f) : v[i];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = s & 1 ? (i < 7 ? v[i + 1 & 7] : 0.0f) : v[i];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = s == 8 ? 0.0f : v[i];
-    } else {
-      typedef __attribute__((ext_vector_type(4))) uint32_t W;
-      W x = __builtin_bit_cast(W, v);
-      uint32_t w[4] = {x[0], x[1], x[2], x[3]};
-      move_down(w, s);
-      x = W{w[0], w[1], w[2], w[3]};
-      v = __builtin_bit_cast(Elem8<DT>, x);
-    }
+    move_units<DT>(v, at - from < 8 ? (int)(at - from) : 8);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

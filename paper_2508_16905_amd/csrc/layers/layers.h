@@ -17,8 +17,8 @@ hipError_t launch_gemm_fp16(Product kind, const GemmPlan& p, const GemmArgs& g, 
 hipError_t launch_gemm_bf16(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream);
 hipError_t launch_gemm_fp32(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream);
 
-// Matrices laid out for the direct form of a product: rows of whole 16-byte units, zeros behind `cols`; fp32 as three bf16 parts,
-// `plane` elements apart.
+// Matrices of fp32 laid out for the wide form of a product: three bf16 parts, `plane` elements apart, rows of whole 16-byte
+// units with zeros behind `cols`.
 struct PackedMatrix {
   const void* src;
   int64_t ld, rows, cols;
@@ -29,7 +29,7 @@ struct PackArgs {
   PackedMatrix m[4];
   int32_t count;
 };
-hipError_t launch_pack(int dtype, const PackArgs& a, hipStream_t stream);
+hipError_t launch_pack(const PackArgs& a, hipStream_t stream);
 
 // The gradient before the activation, and its sums over the rows.
 struct SlopeArgs {

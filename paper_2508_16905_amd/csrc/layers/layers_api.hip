@@ -144,15 +144,17 @@ int pack(const Products& q, char* ws, hipStream_t s) {
       const Operand& o = q.op[i];
       a.m[a.count++] = PackedMatrix{o.p, o.ld, o.rows, o.cols, ws + q.at[i], packed_ld(o), o.rows * packed_ld(o)};
     }
-  return a.count ? hip_status(launch_pack(q.dtype, a, s), "operands laid out") : TRIACCEL_OK;
+  return a.count ? hip_status(launch_pack(a, s), "operands laid out") : TRIACCEL_OK;
 }
-// Operand i for a product: as it was laid out if the product is direct.
-const void* place(const Products& q, int i, bool direct, char* ws, int64_t& ld, int64_t& plane) {
-  const bool anew = direct && q.pack[i];
+// Operand i for a product: as it was laid out if the product is in the wide form.
+const void* place(const Products& q, int i, bool wide, char* ws, int64_t& ld, int64_t& plane) {
+  const bool anew = wide && q.pack[i];
   ld = anew ? packed_ld(q.op[i]) : q.op[i].ld;
   plane = anew ? q.op[i].rows * ld : 0;
   return anew ? ws + q.at[i] : q.op[i].p;
 }
+
+bool is_wide(const GemmPlan& p) { return p.tile == kTileM || p.tile == kTileL; }
 
 struct ForwardPlan {
   Products q;
@@ -166,8 +168,10 @@ ForwardPlan plan_forward(int32_t dtype, Product kind, int64_t rows, int64_t in, 
   if (two) f.q.op[2] = Operand{w2, ldw, out, in};
   f.q.op[3] = Operand{x, ldx, rows, in};
   unsigned need = two ? 14u : 10u;
-  f.g = plan_gemm(dtype == TRIACCEL_FP32, two, pack_us(f.q, need), rows, out, in, 1);
-  if (f.g.tile == kTileS) need = 0;
+  // up to 16 rows: bound by reading the weights (10240 -> 4096 in bf16, one row: 18 us and a second launch of 4 in small tiles)
+  if (rows <= 16) f.g.tile = kTileThin;
+  else f.g = plan_gemm(dtype == TRIACCEL_FP32, two, pack_us(f.q, need), in, rows, out, in, 1);
+  if (!is_wide(f.g)) need = 0;
   lay_out(f.q, 0, need, f.g.partial_bytes);
   return f;
 }
@@ -208,13 +212,13 @@ BackwardPlan plan_backward(const BackwardShape& b, const void* ws) {
   unsigned need_dx = b.wide == 2 ? 7u : 3u, need_dw = 9u, need = 0;
   uint64_t partial = 0;
   if (b.dx && b.rows > 0) {
-    l.dx = plan_gemm(fp32, false, pack_us(q, need_dx), b.rows, b.in, b.out, b.wide);
-    if (l.dx.tile != kTileS) need |= need_dx;
+    l.dx = plan_gemm(fp32, false, pack_us(q, need_dx), b.in < b.out ? b.in : b.out, b.rows, b.in, b.out, b.wide);
+    if (is_wide(l.dx)) need |= need_dx;
     partial = l.dx.partial_bytes;
   }
   if (b.dw) {
-    l.dw = plan_gemm(fp32, false, pack_us(q, need_dw & ~need), b.wide == 2 ? l.width + b.out : b.out, b.in, b.rows, 1);
-    if (l.dw.tile != kTileS) need |= need_dw;
+    l.dw = plan_gemm(fp32, false, pack_us(q, need_dw & ~need), b.in < b.out ? b.in : b.out, b.wide == 2 ? l.width + b.out : b.out, b.in, b.rows, 1);
+    if (is_wide(l.dw)) need |= need_dw;
     if (l.dw.partial_bytes > partial) partial = l.dw.partial_bytes;
   }
   lay_out(q, from, need, partial);
@@ -231,21 +235,21 @@ struct BackwardOut {
 int backward_products(const BackwardShape& b, const BackwardPlan& l, const BackwardOut& o, char* ws, hipStream_t s) {
   TA_TRY(pack(l.q, ws, s));
   if (b.dx && b.rows > 0) {
-    const bool direct = l.dx.tile != kTileS;
+    const bool wide = is_wide(l.dx);
     GemmArgs g{};
-    g.a = place(l.q, 0, direct, ws, g.lda, g.a_plane);
-    g.b = place(l.q, 1, direct, ws, g.ldb, g.b_plane);
-    if (b.wide == 2) g.b2 = place(l.q, 2, direct, ws, g.ldb, g.b_plane);
+    g.a = place(l.q, 0, wide, ws, g.lda, g.a_plane);
+    g.b = place(l.q, 1, wide, ws, g.ldb, g.b_plane);
+    if (b.wide == 2) g.b2 = place(l.q, 2, wide, ws, g.ldb, g.b_plane);
     g.m = (int32_t)b.rows; g.n = (int32_t)b.in; g.seg = (int32_t)b.out; g.nseg = (int32_t)b.wide; g.seg_step = (int32_t)l.width;
     g.partial = (float*)(ws + l.q.partial);
     g.c = o.dx; g.ldc = o.lddx; g.crows = g.csplit = 0x7fffffff; g.c_fp32 = b.dtype == TRIACCEL_FP32;
     TA_TRY(hip_status(run_product(b.dtype, kInputGrad, l.dx, g, s), "gradient of the input"));
   }
   if (b.dw) {  // no rows: the product has no terms and its result is zero
-    const bool direct = l.dw.tile != kTileS;
+    const bool wide = is_wide(l.dw);
     GemmArgs g{};
-    g.a = place(l.q, 0, direct, ws, g.lda, g.a_plane);
-    g.b = place(l.q, 3, direct, ws, g.ldb, g.b_plane);
+    g.a = place(l.q, 0, wide, ws, g.lda, g.a_plane);
+    g.b = place(l.q, 3, wide, ws, g.ldb, g.b_plane);
     g.m = (int32_t)(b.wide == 2 ? l.width + b.out : b.out); g.n = (int32_t)b.in; g.seg = (int32_t)b.rows; g.nseg = 1;
     g.partial = (float*)(ws + l.q.partial);
     g.c = o.dw; g.c2 = o.dw2; g.ldc = o.lddw; g.crows = (int32_t)b.out; g.csplit = b.wide == 2 ? (int32_t)l.width : 0x7fffffff;
@@ -361,10 +365,10 @@ int triaccel_linear(const triaccel_linear_args* a, void* hip_stream) {
   TA_TRY(check_workspace(a->workspace, a->workspace_bytes, f.q.total));
   char* ws = (char*)a->workspace;
   TA_TRY(pack(f.q, ws, (hipStream_t)hip_stream));
-  const bool direct = f.g.tile != kTileS;
+  const bool wide = is_wide(f.g);
   GemmArgs g{};
-  g.a = place(f.q, 3, direct, ws, g.lda, g.a_plane);
-  g.b = place(f.q, 1, direct, ws, g.ldb, g.b_plane);
+  g.a = place(f.q, 3, wide, ws, g.lda, g.a_plane);
+  g.b = place(f.q, 1, wide, ws, g.ldb, g.b_plane);
   g.m = (int32_t)a->rows; g.n = (int32_t)a->out; g.seg = (int32_t)a->in; g.nseg = 1;
   g.partial = (float*)(ws + f.q.partial);
   g.c = a->y; g.ldc = a->ldy; g.pre = a->pre; g.ldpre = a->ldpre;
@@ -435,11 +439,11 @@ int triaccel_gated(const triaccel_gated_args* a, void* hip_stream) {
   TA_TRY(check_workspace(a->workspace, a->workspace_bytes, f.q.total));
   char* ws = (char*)a->workspace;
   TA_TRY(pack(f.q, ws, (hipStream_t)hip_stream));
-  const bool direct = f.g.tile != kTileS;
+  const bool wide = is_wide(f.g);
   GemmArgs g{};
-  g.a = place(f.q, 3, direct, ws, g.lda, g.a_plane);
-  g.b = place(f.q, 1, direct, ws, g.ldb, g.b_plane);
-  g.b2 = place(f.q, 2, direct, ws, g.ldb, g.b_plane);
+  g.a = place(f.q, 3, wide, ws, g.lda, g.a_plane);
+  g.b = place(f.q, 1, wide, ws, g.ldb, g.b_plane);
+  g.b2 = place(f.q, 2, wide, ws, g.ldb, g.b_plane);
   g.m = (int32_t)a->rows; g.n = (int32_t)a->out; g.seg = (int32_t)a->in; g.nseg = 1;
   g.partial = (float*)(ws + f.q.partial);
   g.c = a->h; g.ldc = a->ldh; g.pre = a->gate; g.pre2 = a->up; g.ldpre = a->ldg;

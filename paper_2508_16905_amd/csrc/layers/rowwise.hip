@@ -101,7 +101,6 @@ __global__ __launch_bounds__(1024) void k_column_sums(ColumnSums a) {
 }
 
 // Eight elements of a row per lane, all matrices in one launch.
-template <int DT>
 __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
   int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
 #pragma unroll
@@ -114,16 +113,11 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
       continue;
     }
     const int64_t row = all >> 32 ? id / units : (int64_t)((uint32_t)id / (uint32_t)units), col = (id - row * units) * 8;
-    const Elem8<DT> v = load_edge8<DT>((const Elem<DT>*)m.src + row * m.ld, col, m.cols);
     short* dst = (short*)m.dst + row * m.dst_ld + col;
-    if constexpr (DT == kFP32) {
-      s16x8 part[3];
-      split3(v, part);
+    s16x8 part[3];
+    split3(load_edge8<kFP32>((const float*)m.src + row * m.ld, col, m.cols), part);
 #pragma unroll
-      for (int q = 0; q < 3; ++q) *(TA_GLOBAL s16x8*)(dst + q * m.plane) = part[q];
-    } else {
-      *(TA_GLOBAL s16x8*)dst = __builtin_bit_cast(s16x8, v);
-    }
+    for (int q = 0; q < 3; ++q) *(TA_GLOBAL s16x8*)(dst + q * m.plane) = part[q];
     return;
   }
 }
@@ -163,13 +157,10 @@ hipError_t launch_slope(int dtype, bool gated, const SlopeArgs& a, hipStream_t s
   return hipGetLastError();
 }
 
-hipError_t launch_pack(int dtype, const PackArgs& a, hipStream_t stream) {
+hipError_t launch_pack(const PackArgs& a, hipStream_t stream) {
   int64_t threads = 0;
   for (int i = 0; i < a.count; ++i) threads += a.m[i].rows * (a.m[i].dst_ld / 8);
-  const dim3 grid((uint32_t)ceil_div(threads, 256));
-  if (dtype == kFP16) k_pack<kFP16><<<grid, 256, 0, stream>>>(a);
-  else if (dtype == kBF16) k_pack<kBF16><<<grid, 256, 0, stream>>>(a);
-  else k_pack<kFP32><<<grid, 256, 0, stream>>>(a);
+  k_pack<<<dim3((uint32_t)ceil_div(threads, 256)), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -1,0 +1,119 @@
+// Products of few rows (at most 16): y = act(x W^T + b) ... and the gated pair, for single tokens.
+//
+// Bound by reading the weights once.  A workgroup has 16 columns of the result (16 rows of W, of both matrices if gated) and
+// its wavefronts deal the k among themselves, 32 at a time: no LDS on the way, eight loads of W in flight per lane, the matrix
+// cores for the products (their rate does not matter, but one instruction takes 512 products' worth of work off the vector
+// ALUs), and one sum over the wavefronts at the end.
+#pragma once
+#include "gemm.h"
+
+namespace triaccel {
+namespace layers {
+
+constexpr int kThinRows = 16, kThinCols = 16, kThinWaves = 16;
+
+template <int DT, int EPI>
+struct Thin {
+  static constexpr int kPlanes = DT == kFP32 ? 3 : 1, kMats = EPI == kEpiGated ? 2 : 1;
+  typedef Elem<DT> E;
+
+  static __device__ __forceinline__ void parts(const Elem8<DT>& v, s16x8 (&out)[kPlanes]) {
+    if constexpr (DT == kFP32) split3(v, out);
+    else out[0] = __builtin_bit_cast(s16x8, v);
+  }
+  static __device__ __forceinline__ void multiply(f32x4 (&acc)[kPlanes], const s16x8 (&a)[kPlanes], const s16x8 (&b)[kPlanes]) {
+    if constexpr (DT == kFP32) {
+      acc[2] = mfma<kBF16>(b[2], a[0], acc[2]);
+      acc[1] = mfma<kBF16>(b[1], a[0], acc[1]);
+      acc[0] = mfma<kBF16>(b[0], a[0], acc[0]);
+      acc[2] = mfma<kBF16>(b[0], a[2], acc[2]);
+      acc[1] = mfma<kBF16>(b[0], a[1], acc[1]);
+      acc[2] = mfma<kBF16>(b[1], a[1], acc[2]);
+    } else {
+      acc[0] = mfma<DT>(b[0], a[0], acc[0]);
+    }
+  }
+
+  static __device__ __forceinline__ void run(const GemmArgs& g) {
+    constexpr int kAhead = DT == kFP32 ? 2 : 4;  // steps of 32 k whose loads are in flight
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int waves = (int)blockDim.x >> 6;
+    const int c0 = (int)blockIdx.x * kThinCols;
+    // rows that do not exist are read as the last one and not written
+    const int col = c0 + (lane & 15) < g.n ? c0 + (lane & 15) : g.n - 1, row = (lane & 15) < g.m ? lane & 15 : g.m - 1;
+    const int in = (lane >> 4) * 8;
+    const E* w[kMats];
+    w[0] = (const E*)g.b + (int64_t)col * g.ldb + in;
+    if constexpr (kMats == 2) w[1] = (const E*)g.b2 + (int64_t)col * g.ldb + in;
+    const E* x = (const E*)g.a + (int64_t)row * g.lda + in;
+    f32x4 acc[kMats][kPlanes];
+#pragma unroll
+    for (int i = 0; i < kMats; ++i)
+#pragma unroll
+      for (int q = 0; q < kPlanes; ++q) acc[i][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int whole = g.seg / 32, stride = waves;
+    int s = wave;
+    for (; s + (kAhead - 1) * stride < whole; s += kAhead * stride) {
+      Elem8<DT> vw[kAhead][kMats], vx[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int64_t k = (int64_t)(s + u * stride) * 32;
+#pragma unroll
+        for (int i = 0; i < kMats; ++i) vw[u][i] = load_raw8<DT>(w[i] + k);
+        vx[u] = load_raw8<DT>(x + k);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        s16x8 a[kPlanes], b[kPlanes];
+        parts(vx[u], a);
+#pragma unroll
+        for (int i = 0; i < kMats; ++i) {
+          parts(vw[u][i], b);
+          multiply(acc[i], a, b);
+        }
+      }
+    }
+    for (; s * 32 < g.seg; s += stride) {  // what is left, the end of k among it
+      const int64_t k = (int64_t)s * 32;
+      s16x8 a[kPlanes], b[kPlanes];
+      parts(load_edge8<DT>(x - in, k + in, g.seg), a);
+#pragma unroll
+      for (int i = 0; i < kMats; ++i) {
+        parts(load_edge8<DT>(w[i] - in, k + in, g.seg), b);
+        multiply(acc[i], a, b);
+      }
+    }
+    // the wavefronts' sums, in their order: [wave][mat][row][16 columns]
+    __shared__ float part[kThinWaves][kMats][kThinRows][kThinCols + 4];
+#pragma unroll
+    for (int i = 0; i < kMats; ++i) {
+      if constexpr (DT == kFP32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][0][e] = fmaf(fmaf(acc[i][2][e], 0.00390625f, acc[i][1][e]), 0.00390625f, acc[i][0][e]);
+      }
+      *(f32x4*)&part[wave][i][lane & 15][(lane >> 4) * 4] = acc[i][0];
+    }
+    __syncthreads();
+    const int out_row = (int)threadIdx.x >> 1, out_col = ((int)threadIdx.x & 1) * 8;
+    if (out_row >= g.m || out_row >= kThinRows || c0 + out_col >= g.n) return;
+    float v[8] = {}, u[8] = {};
+    for (int q = 0; q < waves; ++q) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] += part[q][0][out_row][out_col + i];
+        if constexpr (kMats == 2) u[i] += part[q][1][out_row][out_col + i];
+      }
+    }
+    ColumnState state;
+    epi_columns<EPI>(g, c0 + out_col, state);
+    epi_row<DT, EPI>(g, state, out_row, c0 + out_col, 8, v, u);
+  }
+};
+
+template <int DT, int EPI>
+__global__ __launch_bounds__(kThinWaves * 64) void k_thin(GemmArgs g) {
+  Thin<DT, EPI>::run(g);
+}
+
+}  // namespace layers
+}  // namespace triaccel

@@ -70,7 +70,7 @@ def norm(**kw):
     (-1, dict(drop=B.DropoutSpec(1.0, 0, 0, None))), (-1, dict(drop=B.DropoutSpec(-0.1, 0, 0, None))), (-1, dict(drop=B.DropoutSpec(float("nan"), 0, 0, None))),
     (-2, dict(dtype=3)), (-2, dict(bias=ADDRESS, bias_dtype=7)), (-4, dict(x=None)), (-4, dict(weight=None)), (-4, dict(y=None)),
     (-5, dict(x=ADDRESS + 1)), (-5, dict(pre=ADDRESS + 1, ldpre=8)), (-5, dict(drop=B.DropoutSpec(0.5, 0, 0, ADDRESS + 4))),
-    (-1, dict(residual=ADDRESS, ldr=7)), (-1, dict(in_=1 << 20, ldx=1 << 20, ldw=1 << 20)),  # the last: no workspace for a long k
+    (-1, dict(residual=ADDRESS, ldr=7)), (-1, dict(rows=64, in_=1 << 20, ldx=1 << 20, ldw=1 << 20)),  # the last: no workspace for a long k
 ])
 def test_linear_refuses(lib, code, change):
     assert lib.triaccel_linear(C.byref(linear(**change)), None) == code
