@@ -765,11 +765,13 @@ __global__ __launch_bounds__(G::kThreads) void k_gemm(GemmArgs g) {
 // The tiles of the result whose k was shared: eight columns of a row per thread, the shares in order, then the epilogue.
 template <typename G>
 __global__ __launch_bounds__(256) void k_join(GemmArgs g) {
-  constexpr int kGroups = G::kCols / 8, kPer = G::BM * kGroups / 256;  // workgroups of a tile
-  const int tile = blockIdx.x / kPer, id = blockIdx.x % kPer * 256 + threadIdx.x;
+  constexpr uint32_t kGroups = G::kCols / 8, kPer = G::BM * kGroups;  // threads of a tile
+  const uint32_t all = blockIdx.x * 256u + threadIdx.x;
+  const int tile = (int)(all / kPer), id = (int)(all % kPer);
+  if (tile >= g.tiles_m * g.tiles_n - g.whole) return;
   int tm, tn;
   tile_of(g, g.whole + tile, tm, tn);
-  const int in_row = id / kGroups, in_col = id % kGroups * 8;
+  const int in_row = id / (int)kGroups, in_col = id % (int)kGroups * 8;
   const int64_t row = G::origin(tm * G::BM, g.m, G::BM) + in_row;
   int64_t col = G::origin(tn * G::kCols, g.n, G::kCols) + in_col;
   const int over = (int)(tn * G::kCols - col);

@@ -14,7 +14,7 @@ hipError_t launch_with(const GemmPlan& p, const GemmArgs& g, hipStream_t stream)
   k_gemm<G><<<dim3((uint32_t)(p.whole + rest * p.splits)), G::kThreads, 0, stream>>>(g);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || rest == 0) return e;
-  k_join<G><<<dim3((uint32_t)(rest * (G::BM * G::kCols / 8 / 256))), 256, 0, stream>>>(g);
+  k_join<G><<<dim3((uint32_t)ceil_div(rest * (G::BM * G::kCols / 8), 256)), 256, 0, stream>>>(g);
   return hipGetLastError();
 }
 
@@ -30,6 +30,10 @@ hipError_t launch_product(const GemmPlan& p, GemmArgs g, hipStream_t stream) {
   if (p.tile == kTileS) {
     if (p.groups > 1) return launch_with<Gemm<DT, LA, LB, 64, 64, 2, 2, kGroups, EPI, kStaged>>(p, g, stream);
     return launch_with<Gemm<DT, LA, LB, 64, 64, 2, 2, 1, EPI, kStaged>>(p, g, stream);
+  }
+  if (p.tile == kTileX) {
+    if (p.groups > 1) return launch_with<Gemm<DT, LA, LB, 32, 32, 2, 1, 4, EPI, kStaged>>(p, g, stream);
+    return launch_with<Gemm<DT, LA, LB, 32, 32, 2, 1, 1, EPI, kStaged>>(p, g, stream);
   }
   if constexpr (DT != kFP32) {
     if (p.tile == kTileL) return launch_with<Gemm<DT, LA, LB, 256, 256, 2, 2, 1, EPI, kWide>>(p, g, stream);

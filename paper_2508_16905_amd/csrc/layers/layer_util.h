@@ -129,22 +129,30 @@ __device__ __forceinline__ void store1_of(int dtype, void* base, int64_t at, flo
 }
 
 // ---- fp32 in three parts, for the matrix cores (gemm.h) ---
-// Rounded to bf16; cut off instead where rounding would make an infinity of a number.
-__device__ __forceinline__ uint32_t part_bits(float x) {
-  const uint32_t b = f32_to_bf16_bits(x);
-  return (b & 0x7fffu) == 0x7f80u ? f2u(x) >> 16 : b;
-}
-// fp32 -> three bf16 parts.  A rest is below 2^120 and its multiple below 2^128; what is not finite has no rest.
+// Each part is the rest so far, 256 times larger, rounded to bf16.  The first two are held to bf16's largest number, so that
+// rounding makes no infinity of a number; the last one then cannot overflow (a rest has 16 bits, its own rest 8), and takes
+// over what is infinite or not a number.
 __device__ __forceinline__ void split3(const Elem8<kFP32>& v, s16x8 (&out)[3]) {
+  typedef __attribute__((ext_vector_type(2))) float F2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 B2;
+  typedef __attribute__((ext_vector_type(4))) uint32_t U4;
+  constexpr float kMost = 0x1.fep127f;
+  const auto round2 = [](float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector((F2{a, b}), B2)); };
+  U4 part[3];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t h = part_bits(v[i]);
-    const float r = __builtin_isfinite(v[i]) ? (v[i] - bf16_bits_to_f32(h)) * 256.0f : 0.0f;
-    const uint32_t m = part_bits(r);
-    out[0][i] = (short)h;
-    out[1][i] = (short)m;
-    out[2][i] = (short)part_bits((r - bf16_bits_to_f32(m)) * 256.0f);
+  for (int i = 0; i < 4; ++i) {
+    float a = v[2 * i], b = v[2 * i + 1];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const uint32_t p = round2(__builtin_amdgcn_fmed3f(a, -kMost, kMost), __builtin_amdgcn_fmed3f(b, -kMost, kMost));
+      part[q][i] = p;
+      a = (a - u2f(p << 16)) * 256.0f;
+      b = (b - u2f(p & 0xffff0000u)) * 256.0f;
+    }
+    part[2][i] = round2(a, b);
   }
+#pragma unroll
+  for (int q = 0; q < 3; ++q) out[q] = __builtin_bit_cast(s16x8, part[q]);
 }
 
 // ---- activations ------------------------------------------------------------------------------------------------
