@@ -135,7 +135,7 @@ double pack_us(const Products& q, unsigned need) {
     if (q.op[i].cols >= (1 << 21) || q.op[i].ld >= (1 << 21) || q.op[i].rows * q.op[i].cols >= (int64_t)1 << 32) return 1e30;
     bytes += packed_bytes(q.op[i]) / 6 * 10;
   }
-  return q.dtype == TRIACCEL_FP32 && bytes ? 6.0 + (double)bytes / 4.0e6 : 0.0;
+  return q.dtype == TRIACCEL_FP32 && bytes ? 5.0 + (double)bytes / 4.0e6 : 0.0;
 }
 int pack(const Products& q, char* ws, hipStream_t s) {
   PackArgs a{};
@@ -209,17 +209,31 @@ BackwardPlan plan_backward(const BackwardShape& b, const void* ws) {
   if (b.wide == 2) q.op[2] = Operand{b.w2, b.ldw, b.out, b.in};
   q.op[3] = Operand{b.x, b.ldx, b.rows, b.in};
   const bool fp32 = b.dtype == TRIACCEL_FP32;
-  unsigned need_dx = b.wide == 2 ? 7u : 3u, need_dw = 9u, need = 0;
+  // each product in the wide form or not: what is laid out for both is paid for once
+  const unsigned need_dx = b.wide == 2 ? 7u : 3u, need_dw = 9u;
+  const int64_t shortest = b.in < b.out ? b.in : b.out;
+  const bool dx = b.dx && b.rows > 0;
+  unsigned need = 0;
   uint64_t partial = 0;
-  if (b.dx && b.rows > 0) {
-    l.dx = plan_gemm(fp32, false, pack_us(q, need_dx), b.in < b.out ? b.in : b.out, b.rows, b.in, b.out, b.wide);
-    if (is_wide(l.dx)) need |= need_dx;
-    partial = l.dx.partial_bytes;
-  }
-  if (b.dw) {
-    l.dw = plan_gemm(fp32, false, pack_us(q, need_dw & ~need), b.in < b.out ? b.in : b.out, b.wide == 2 ? l.width + b.out : b.out, b.in, b.rows, 1);
-    if (is_wide(l.dw)) need |= need_dw;
-    if (l.dw.partial_bytes > partial) partial = l.dw.partial_bytes;
+  double best = -1.0;
+  for (int form = 0; form < 4; ++form) {
+    GemmPlan x{}, w{};
+    unsigned needs = 0;
+    if (dx) {
+      x = plan_gemm(fp32, false, form & 1 ? 0.0 : 1e30, shortest, b.rows, b.in, b.out, b.wide);
+      if (is_wide(x)) needs |= need_dx;
+    }
+    if (b.dw) {
+      w = plan_gemm(fp32, false, form & 2 ? 0.0 : 1e30, shortest, b.wide == 2 ? l.width + b.out : b.out, b.in, b.rows, 1);
+      if (is_wide(w)) needs |= need_dw;
+    }
+    const double us = x.us + w.us + pack_us(q, needs);
+    if (best >= 0.0 && us >= best) continue;
+    best = us;
+    need = needs;
+    l.dx = x;
+    l.dw = w;
+    partial = x.partial_bytes > w.partial_bytes ? x.partial_bytes : w.partial_bytes;
   }
   lay_out(q, from, need, partial);
   l.total = q.total;
