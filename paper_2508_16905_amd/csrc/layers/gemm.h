@@ -176,18 +176,19 @@ __device__ __forceinline__ int on_xcd(int id, int total) {
   return xcd * per + (xcd < more ? xcd : more) + (id >> 3);
 }
 
-template <int DT_, int LA, int LB, int BM_, int BN_, int WR, int WC, int KG, int EPI_, int FORM>
+template <int DT_, int LA, int LB, int BM_, int BN_, int WR, int WC, int KG, int EPI_, int FORM, int AP = 1>
 struct Gemm {
   static constexpr bool WIDE = FORM == kWide;
   static constexpr int DT = DT_, BM = BM_, BN = BN_, EPI = EPI_;
-  static constexpr int kPlanes = DT == kFP32 ? 3 : 1;
+  // Parts of an operand in LDS.  AP = 2 (16 bits, staged): A comes in two parts, a value and what rounding took from it.
+  static constexpr int kPlanes = DT == kFP32 ? 3 : 1, kPartsA = DT == kFP32 ? 3 : AP;
   static constexpr int BK = DT == kFP32 ? 32 : 64;
   static constexpr int NT = WR * WC * 64;                 // threads of a group
   static constexpr int kThreads = NT * KG;
   static constexpr int FM = BM / WR / 16, FN = BN / WC / 16;
   static constexpr int kAUnits = BM * BK / 8, kBUnits = BN * BK / 8;
   static constexpr int TA = kAUnits / NT, TB = kBUnits / NT;
-  static constexpr int kTile = kPlanes * (BM + BN) * BK;  // elements of one buffer
+  static constexpr int kTile = (kPartsA * BM + kPlanes * BN) * BK;  // elements of one buffer
   static constexpr int kSlabCols = FN * 16, kSlabLd = kSlabCols + 4;
   static constexpr int kRound = FM < 4 ? FM : 4;          // fragments of rows that a wavefront's slab holds at a time
   static constexpr int kSlab = 16 * kRound * kSlabLd;     // floats of a wavefront
@@ -334,10 +335,10 @@ struct Gemm {
     }
   }
   template <int L, int R, int T, bool IS_B>
-  static __device__ __forceinline__ void fetch(const GemmArgs& g, const At& w, int rows, const int64_t (&off)[T], Elem8<DT> (&out)[T], uint32_t tid) {
+  static __device__ __forceinline__ void fetch(const GemmArgs& g, const At& w, int rows, const int64_t (&off)[T], int64_t plane, Elem8<DT> (&out)[T], uint32_t tid) {
     const int64_t ld = IS_B ? g.ldb : g.lda;
     const int64_t k0 = (IS_B ? 0 : w.seg * (int64_t)g.seg_step) + w.k0;
-    const char* base = (const char*)((const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a) + (L == KC ? k0 : k0 * ld));
+    const char* base = (const char*)((const E*)(IS_B ? (w.seg ? g.b2 : g.b) : g.a) + (L == KC ? k0 : k0 * ld) + plane);
     const char* base2 = (const char*)((const E*)g.b2 + k0);
     const int len = L == KC ? g.seg : rows;
 #pragma unroll
@@ -405,10 +406,10 @@ struct Gemm {
 
   // --- products of 32 k ---
   struct Frags {
-    s16x8 a[FM][kPlanes], b[FN][kPlanes];
+    s16x8 a[FM][kPartsA], b[FN][kPlanes];
   };
   static __device__ __forceinline__ void read(Frags& f, const short* tile, int k0, int wm, int wn, int lane) {
-    const short* tb = tile + kPlanes * BM * BK;
+    const short* tb = tile + kPartsA * BM * BK;
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -416,7 +417,7 @@ struct Gemm {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int q = 0; q < kPlanes; ++q) f.a[i][q] = fragment<LA, BM, BK>(tile + q * BM * BK, wm * FM * 16 + i * 16, k0, lane);
+      for (int q = 0; q < kPartsA; ++q) f.a[i][q] = fragment<LA, BM, BK>(tile + q * BM * BK, wm * FM * 16 + i * 16, k0, lane);
   }
   template <int I0, int I1>
   static __device__ __forceinline__ void multiply(Acc& acc, const Frags& f) {
@@ -434,6 +435,7 @@ struct Gemm {
           acc[1][i][j] = mfma<kBF16>(b[0], a[1], acc[1][i][j]);
           acc[2][i][j] = mfma<kBF16>(b[1], a[1], acc[2][i][j]);
         } else {
+          if constexpr (AP == 2) acc[0][i][j] = mfma<DT>(b[0], a[1], acc[0][i][j]);
           acc[0][i][j] = mfma<DT>(b[0], a[0], acc[0][i][j]);
         }
       }
@@ -655,14 +657,15 @@ struct Gemm {
   // kAhead tiles of a group are on their way to its registers.
   static constexpr int kAhead = 3;
   static __device__ __forceinline__ void staged_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int kg, int tid, int wm, int wn, int lane) {
-    Elem8<DT> ra[kAhead][TA], rb[kAhead][TB];
+    Elem8<DT> ra[kAhead][AP][TA], rb[kAhead][TB];
     int64_t off_a[TA], off_b[TB];
     offsets<LA, BM, TA, false>(g, r0, g.m, off_a, tid);
     offsets<LB, BN, TB, true>(g, c0, g.n, off_b, tid);
     const auto load = [&](int kt, int set) {
       const At w = at(g, kt);
-      fetch<LA, BM, TA, false>(g, w, g.m, off_a, ra[set], tid);
-      fetch<LB, BN, TB, true>(g, w, g.n, off_b, rb[set], tid);
+#pragma unroll
+      for (int q = 0; q < AP; ++q) fetch<LA, BM, TA, false>(g, w, g.m, off_a, q * g.a_plane, ra[set][q], tid);
+      fetch<LB, BN, TB, true>(g, w, g.n, off_b, 0, rb[set], tid);
     };
     short* mine = lds + kg * 2 * kTile;
     int now = first + kg, buf = 0;
@@ -677,10 +680,13 @@ struct Gemm {
         short* to = mine + buf * kTile;
         if (now < last) {
           const At w = at(g, now);
-          settle<LA, BM, TA, false>(g, w, r0, g.m, ra[i], tid);
+#pragma unroll
+          for (int q = 0; q < AP; ++q) {
+            settle<LA, BM, TA, false>(g, w, r0, g.m, ra[i][q], tid);
+            place<LA, BM, TA>(ra[i][q], to + q * BM * BK, tid);
+          }
           settle<LB, BN, TB, true>(g, w, c0, g.n, rb[i], tid);
-          place<LA, BM, TA>(ra[i], to, tid);
-          place<LB, BN, TB>(rb[i], to + kPlanes * BM * BK, tid);
+          place<LB, BN, TB>(rb[i], to + kPartsA * BM * BK, tid);
         }
         meet();
         if (now + kAhead * KG < last) load(now + kAhead * KG, i);
@@ -699,18 +705,19 @@ struct Gemm {
     }
   }
 
-  static __device__ __forceinline__ void run(const GemmArgs& g, short* lds) {
+  // `block`: the number of this workgroup among those of the product.
+  static __device__ __forceinline__ void run(const GemmArgs& g, short* lds, int block) {
     const int tid = threadIdx.x % NT, lane = tid & 63;
     const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / NT);
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WC, wn = wave % WC;
     const int all = g.seg > 0 ? (g.seg + BK - 1) / BK * g.nseg : 0;
     int t, first = 0, last = all;
     float* partial = nullptr;
-    if ((int)blockIdx.x < g.whole) {
-      t = on_xcd(blockIdx.x, g.whole);
+    if (block < g.whole) {
+      t = on_xcd(block, g.whole);
     } else {
       const int rest = g.tiles_m * g.tiles_n - g.whole;
-      const int lin = on_xcd((int)blockIdx.x - g.whole, rest * g.splits);
+      const int lin = on_xcd(block - g.whole, rest * g.splits);
       t = g.whole + lin / g.splits;
       first = lin % g.splits * g.per_split;
       last = first + g.per_split < all ? first + g.per_split : all;
@@ -759,7 +766,20 @@ struct Gemm {
 template <typename G>
 __global__ __launch_bounds__(G::kThreads) void k_gemm(GemmArgs g) {
   __shared__ __attribute__((aligned(16))) short lds[G::kLdsBytes / 2];
-  G::run(g, lds);
+  G::run(g, lds, (int)blockIdx.x);
+}
+
+// Two products in one launch, for the gradients of a small layer: the first workgroups have the one, the others the other.
+struct PairArgs {
+  GemmArgs x, w;
+  int32_t first;  // workgroups of x
+};
+template <typename GX, typename GW>
+__global__ __launch_bounds__(GX::kThreads) void k_pair(PairArgs p) {
+  static_assert(GX::kThreads == GW::kThreads, "one workgroup size");
+  __shared__ __attribute__((aligned(16))) short lds[(GX::kLdsBytes > GW::kLdsBytes ? GX::kLdsBytes : GW::kLdsBytes) / 2];
+  if ((int)blockIdx.x < p.first) GX::run(p.x, lds, (int)blockIdx.x);
+  else GW::run(p.w, lds, (int)blockIdx.x - p.first);
 }
 
 // The tiles of the result whose k was shared: eight columns of a row per thread, the shares in order, then the epilogue.

@@ -8,5 +8,9 @@ hipError_t launch_gemm_fp16(Product kind, const GemmPlan& p, const GemmArgs& g, 
   return launch_any<kFP16>(kind, p, g, stream);
 }
 
+hipError_t launch_pair_fp16(bool two_parts, const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x, const GemmArgs& w, hipStream_t stream) {
+  return launch_pair_any<kFP16>(two_parts, px, pw, x, w, stream);
+}
+
 }  // namespace layers
 }  // namespace triaccel

@@ -41,6 +41,40 @@ hipError_t launch_product(const GemmPlan& p, GemmArgs g, hipStream_t stream) {
   return launch_with<Gemm<DT, LA, LB, 128, 128, 2, 2, 1, EPI, kWide>>(p, g, stream);
 }
 
+// The gradients of the input and of the weights in one launch; AP: parts of dz.
+template <int DT, int AP>
+hipError_t launch_both(const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x, const GemmArgs& w, hipStream_t stream) {
+  PairArgs p{x, w, px.tiles_m * px.tiles_n};
+  const auto fill = [](GemmArgs& g, const GemmPlan& q) {
+    g.tiles_m = q.tiles_m;
+    g.tiles_n = q.tiles_n;
+    g.whole = q.tiles_m * q.tiles_n;
+    g.splits = 1;
+    g.per_split = q.per_split;
+  };
+  fill(p.x, px);
+  fill(p.w, pw);
+  const dim3 grid((uint32_t)(p.x.whole + p.w.whole));
+  if (px.tile == kTileX) {
+    typedef Gemm<DT, KC, KS, 32, 32, 2, 1, 4, kEpiStore, kStaged, AP> GX;
+    typedef Gemm<DT, KS, KS, 32, 32, 2, 1, 4, kEpiStore, kStaged, AP> GW;
+    k_pair<GX, GW><<<grid, GX::kThreads, 0, stream>>>(p);
+  } else {
+    constexpr int kGroups = DT == kFP32 ? 2 : 3;
+    typedef Gemm<DT, KC, KS, 64, 64, 2, 2, kGroups, kEpiStore, kStaged, AP> GX;
+    typedef Gemm<DT, KS, KS, 64, 64, 2, 2, kGroups, kEpiStore, kStaged, AP> GW;
+    k_pair<GX, GW><<<grid, GX::kThreads, 0, stream>>>(p);
+  }
+  return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_pair_any(bool two_parts, const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x, const GemmArgs& w, hipStream_t stream) {
+  if constexpr (DT != kFP32) {
+    if (two_parts) return launch_both<DT, 2>(px, pw, x, w, stream);
+  }
+  return launch_both<DT, 1>(px, pw, x, w, stream);
+}
+
 template <int DT, int EPI>
 hipError_t launch_thin(const GemmArgs& g, hipStream_t stream) {
   // a wavefront has two steps of 32 k at least, so that short k do not pay for sixteen wavefronts

@@ -69,6 +69,26 @@ inline GemmPlan plan_tile(int tile, bool fp32, bool gated, int64_t m, int64_t n,
   return p;
 }
 
+// All tiles of one staged product, none of them shared.
+inline GemmPlan plan_whole(int tile, bool fp32, bool gated, int64_t m, int64_t n, int64_t seg, int64_t nseg) {
+  GemmPlan p = plan_tile(tile, fp32, gated, m, n, seg, nseg);
+  p.whole = p.tiles_m * p.tiles_n;
+  p.splits = 1;
+  p.per_split = (int32_t)(seg > 0 ? ceil_div(seg, fp32 ? 32 : 64) * nseg : 1);
+  p.partial_bytes = 0;
+  return p;
+}
+// Two such products in one launch: their tiles' bytes over the CUs, at least the longer tile, and what each further round of
+// workgroups takes to begin and end (fp32 and two parts of dz leave room for one on a CU).
+inline double pair_us(int tile, bool fp32, int parts, const GemmPlan& x, const GemmPlan& w) {
+  const double edge = tile == kTileX ? 32 : 64, kb = edge * (fp32 ? 2 * 32 * 4 : (1 + parts) * 64 * 2) / 1024.0;
+  const double rate = !fp32 ? 38.0 : tile == kTileX ? 28.0 : 18.0;
+  const double tx = (double)x.tiles_m * x.tiles_n, tw = (double)w.tiles_m * w.tiles_n;
+  const double all = kb * (tx * x.per_split + tw * w.per_split) / 256.0, one = kb * (double)(x.per_split > w.per_split ? x.per_split : w.per_split);
+  const double rounds = (tx + tw) / (fp32 || parts > 1 || tile == kTileS ? 256.0 : 512.0);
+  return 4.0 + (rounds > 1.0 ? 2.5 * (rounds - 1.0) : 0.0) + (all > one ? all : one) / rate;
+}
+
 // m x n results (gated: n columns of two products), k = nseg segments of seg.  `pack_us`: what it takes to lay the operands out
 // for the wide form.
 // `shortest`: the shortest row of an operand.

@@ -17,6 +17,11 @@ hipError_t launch_gemm_fp16(Product kind, const GemmPlan& p, const GemmArgs& g, 
 hipError_t launch_gemm_bf16(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream);
 hipError_t launch_gemm_fp32(Product kind, const GemmPlan& p, const GemmArgs& g, hipStream_t stream);
 
+// Both gradients of a small layer in one launch; two_parts: dz lies in two parts, dz_plane elements apart (16 bits).
+hipError_t launch_pair_fp16(bool two_parts, const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x, const GemmArgs& w, hipStream_t stream);
+hipError_t launch_pair_bf16(bool two_parts, const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x, const GemmArgs& w, hipStream_t stream);
+hipError_t launch_pair_fp32(bool two_parts, const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x, const GemmArgs& w, hipStream_t stream);
+
 // Matrices of fp32 laid out for the wide form of a product: three bf16 parts, `plane` elements apart, rows of whole 16-byte
 // units with zeros behind `cols`.
 struct PackedMatrix {
@@ -37,7 +42,10 @@ struct SlopeArgs {
   int64_t lddy, ldg;
   int64_t rows, cols, width;    // width: cols rounded up to the columns that dz has in the workspace
   void *dz;                     // NULL: sums only.  gated: rows x (2 width), dg and du side by side
+  int64_t rest;                 // > 0: what rounding to 16 bits takes from dz goes `rest` elements behind it
   float *sums;                  // [blocks][cols] (gated: [blocks][2 cols]), or NULL
+  void *bias, *bias2;           // one block: the sums themselves, of type bias_dtype, or NULL
+  int32_t bias_dtype;
   int64_t rows_per_block;
   int32_t act, blocks;
   const Drop* drop;             // linear only (host pointer)

@@ -96,6 +96,11 @@ hipError_t run_product(int32_t dtype, Product kind, const GemmPlan& p, const Gem
          : dtype == TRIACCEL_BF16 ? launch_gemm_bf16(kind, p, g, s) : launch_gemm_fp32(kind, p, g, s);
 }
 
+hipError_t run_pair(int32_t dtype, bool two_parts, const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x, const GemmArgs& w, hipStream_t s) {
+  return dtype == TRIACCEL_FP16 ? launch_pair_fp16(two_parts, px, pw, x, w, s)
+         : dtype == TRIACCEL_BF16 ? launch_pair_bf16(two_parts, px, pw, x, w, s) : launch_pair_fp32(two_parts, px, pw, x, w, s);
+}
+
 // An operand as the caller (or the workspace) has it.
 struct Operand {
   const void* p;
@@ -185,6 +190,8 @@ struct BackwardPlan {
   int64_t rows_per_block;
   Products q;
   GemmPlan dx, dw;
+  bool pair;                // both products in one launch
+  int64_t rest;             // of dz in two parts, elements between them; else 0
 };
 struct BackwardShape {
   int32_t dtype;
@@ -193,14 +200,37 @@ struct BackwardShape {
   const void *dy, *x, *w, *w2;
   int64_t lddy, ldx, ldw;
 };
+int64_t weight_rows(const BackwardShape& b, const BackwardPlan& l) { return b.wide == 2 ? l.width + b.out : b.out; }
+// Whether both gradients go in one launch, in small tiles: where this is no longer than what the launches of the other forms
+// would take (three more of them at 5 us on the average).
+bool pair_plan(const BackwardShape& b, BackwardPlan& l) {
+  if (!b.dx || !b.dw || b.rows < 1 || b.in < 8 || b.out < 8) return false;
+  const bool fp32 = b.dtype == TRIACCEL_FP32;
+  double best = 1e30;
+  for (const int tile : {kTileX, kTileS}) {
+    const GemmPlan x = plan_whole(tile, fp32, false, b.rows, b.in, b.out, b.wide), w = plan_whole(tile, fp32, false, weight_rows(b, l), b.in, b.rows, 1);
+    const double us = pair_us(tile, fp32, b.slope ? 2 : 1, x, w);
+    if (us >= best) continue;
+    best = us;
+    l.dx = x;
+    l.dw = w;
+  }
+  const GemmPlan x = plan_gemm(fp32, false, 5.0, 8, b.rows, b.in, b.out, b.wide), w = plan_gemm(fp32, false, 5.0, 8, weight_rows(b, l), b.in, b.rows, 1);
+  return best <= x.us + w.us + 5.0;
+}
 BackwardPlan plan_backward(const BackwardShape& b, const void* ws) {
   BackwardPlan l{};
   l.width = (b.out + 7) / 8 * 8;
-  // 64 rows a workgroup, more where that makes over 128 blocks (their sums are added up by one workgroup per 64 columns)
-  l.rows_per_block = 64;
-  if (ceil_div(b.rows, l.rows_per_block) > 128) l.rows_per_block = ceil_div(b.rows, 128);
+  l.pair = pair_plan(b, l);
+  // Blocks of rows of the kernel that makes dz and the sums of its columns, eight rows at a time: enough workgroups of 256
+  // columns to fill the card, at most 512 blocks.  Up to 64 rows are one block, whose sums need no second kernel.
+  const int64_t want = ceil_div(2048, ceil_div(l.width, 256));
+  l.rows_per_block = ceil_div(ceil_div(b.rows, want < 512 ? want : 512), 8) * 8;
+  if (b.rows <= 64 || l.rows_per_block < 8) l.rows_per_block = 64;
   l.blocks = (int32_t)ceil_div(b.rows, l.rows_per_block);
-  l.sums = b.slope ? padded((uint64_t)b.rows * (uint64_t)(b.wide * l.width) * (uint64_t)bytes_of(b.dtype)) : 0;
+  const int64_t dz = b.slope ? b.rows * b.wide * l.width : 0;
+  l.rest = l.pair && b.dtype != TRIACCEL_FP32 ? dz : 0;
+  l.sums = padded((uint64_t)(dz + l.rest) * (uint64_t)bytes_of(b.dtype));
   const uint64_t from = l.sums + (b.sums ? padded((uint64_t)l.blocks * (uint64_t)(b.wide * b.out) * 4u) : 0);
   Products& q = l.q;
   q.dtype = b.dtype;
@@ -209,6 +239,11 @@ BackwardPlan plan_backward(const BackwardShape& b, const void* ws) {
   if (b.wide == 2) q.op[2] = Operand{b.w2, b.ldw, b.out, b.in};
   q.op[3] = Operand{b.x, b.ldx, b.rows, b.in};
   const bool fp32 = b.dtype == TRIACCEL_FP32;
+  if (l.pair) {
+    lay_out(q, from, 0, 0);
+    l.total = q.total;
+    return l;
+  }
   // each product in the wide form or not: what is laid out for both is paid for once
   const unsigned need_dx = b.wide == 2 ? 7u : 3u, need_dw = 9u;
   const int64_t shortest = b.in < b.out ? b.in : b.out;
@@ -224,7 +259,7 @@ BackwardPlan plan_backward(const BackwardShape& b, const void* ws) {
       if (is_wide(x)) needs |= need_dx;
     }
     if (b.dw) {
-      w = plan_gemm(fp32, false, form & 2 ? 0.0 : 1e30, shortest, b.wide == 2 ? l.width + b.out : b.out, b.in, b.rows, 1);
+      w = plan_gemm(fp32, false, form & 2 ? 0.0 : 1e30, shortest, weight_rows(b, l), b.in, b.rows, 1);
       if (is_wide(w)) needs |= need_dw;
     }
     const double us = x.us + w.us + pack_us(q, needs);
@@ -248,28 +283,32 @@ struct BackwardOut {
 };
 int backward_products(const BackwardShape& b, const BackwardPlan& l, const BackwardOut& o, char* ws, hipStream_t s) {
   TA_TRY(pack(l.q, ws, s));
+  GemmArgs x{}, w{};
   if (b.dx && b.rows > 0) {
     const bool wide = is_wide(l.dx);
-    GemmArgs g{};
-    g.a = place(l.q, 0, wide, ws, g.lda, g.a_plane);
-    g.b = place(l.q, 1, wide, ws, g.ldb, g.b_plane);
-    if (b.wide == 2) g.b2 = place(l.q, 2, wide, ws, g.ldb, g.b_plane);
-    g.m = (int32_t)b.rows; g.n = (int32_t)b.in; g.seg = (int32_t)b.out; g.nseg = (int32_t)b.wide; g.seg_step = (int32_t)l.width;
-    g.partial = (float*)(ws + l.q.partial);
-    g.c = o.dx; g.ldc = o.lddx; g.crows = g.csplit = 0x7fffffff; g.c_fp32 = b.dtype == TRIACCEL_FP32;
-    TA_TRY(hip_status(run_product(b.dtype, kInputGrad, l.dx, g, s), "gradient of the input"));
+    x.a = place(l.q, 0, wide, ws, x.lda, x.a_plane);
+    x.b = place(l.q, 1, wide, ws, x.ldb, x.b_plane);
+    if (b.wide == 2) x.b2 = place(l.q, 2, wide, ws, x.ldb, x.b_plane);
+    x.m = (int32_t)b.rows; x.n = (int32_t)b.in; x.seg = (int32_t)b.out; x.nseg = (int32_t)b.wide; x.seg_step = (int32_t)l.width;
+    x.partial = (float*)(ws + l.q.partial);
+    x.c = o.dx; x.ldc = o.lddx; x.crows = x.csplit = 0x7fffffff; x.c_fp32 = b.dtype == TRIACCEL_FP32;
   }
   if (b.dw) {  // no rows: the product has no terms and its result is zero
     const bool wide = is_wide(l.dw);
-    GemmArgs g{};
-    g.a = place(l.q, 0, wide, ws, g.lda, g.a_plane);
-    g.b = place(l.q, 3, wide, ws, g.ldb, g.b_plane);
-    g.m = (int32_t)(b.wide == 2 ? l.width + b.out : b.out); g.n = (int32_t)b.in; g.seg = (int32_t)b.rows; g.nseg = 1;
-    g.partial = (float*)(ws + l.q.partial);
-    g.c = o.dw; g.c2 = o.dw2; g.ldc = o.lddw; g.crows = (int32_t)b.out; g.csplit = b.wide == 2 ? (int32_t)l.width : 0x7fffffff;
-    g.c_fp32 = o.dw_dtype == TRIACCEL_FP32;
-    TA_TRY(hip_status(run_product(b.dtype, kWeightGrad, l.dw, g, s), "gradient of the weights"));
+    w.a = place(l.q, 0, wide, ws, w.lda, w.a_plane);
+    w.b = place(l.q, 3, wide, ws, w.ldb, w.b_plane);
+    w.m = (int32_t)weight_rows(b, l); w.n = (int32_t)b.in; w.seg = (int32_t)b.rows; w.nseg = 1;
+    w.partial = (float*)(ws + l.q.partial);
+    w.c = o.dw; w.c2 = o.dw2; w.ldc = o.lddw; w.crows = (int32_t)b.out; w.csplit = b.wide == 2 ? (int32_t)l.width : 0x7fffffff;
+    w.c_fp32 = o.dw_dtype == TRIACCEL_FP32;
   }
+  if (l.pair) {
+    const bool parts = l.rest > 0;
+    if (parts) x.a_plane = w.a_plane = l.rest;
+    return hip_status(run_pair(b.dtype, parts, l.dx, l.dw, x, w, s), "gradients of the input and of the weights");
+  }
+  if (x.m) TA_TRY(hip_status(run_product(b.dtype, kInputGrad, l.dx, x, s), "gradient of the input"));
+  if (b.dw) TA_TRY(hip_status(run_product(b.dtype, kWeightGrad, l.dw, w, s), "gradient of the weights"));
   return TRIACCEL_OK;
 }
 
@@ -418,11 +457,14 @@ int triaccel_linear_backward(const triaccel_linear_backward_args* a, void* hip_s
     q.dy = a->dy; q.lddy = a->lddy; q.gate = a->pre; q.ldg = a->ldpre;
     q.rows = a->rows; q.cols = a->out; q.width = l.width;
     q.dz = slope ? ws : nullptr;
-    q.sums = a->dbias ? (float*)(ws + l.sums) : nullptr;
+    q.rest = l.rest;
+    if (l.blocks > 1) q.sums = a->dbias ? (float*)(ws + l.sums) : nullptr;
+    else q.bias = a->dbias;
+    q.bias_dtype = a->dbias_dtype;
     q.rows_per_block = l.rows_per_block; q.blocks = l.blocks; q.act = a->act; q.drop = &drop;
     TA_TRY(hip_status(launch_slope(a->dtype, false, q, s), "gradient before the activation"));
   }
-  if (a->dbias) {
+  if (a->dbias && l.blocks != 1) {
     ColumnSums c{(const float*)(ws + l.sums), a->out, a->out, l.blocks, 1, a->dbias_dtype, {a->dbias}};
     TA_TRY(hip_status(launch_column_sums(c, s), "gradient of the bias"));
   }
@@ -499,11 +541,18 @@ int triaccel_gated_backward(const triaccel_gated_backward_args* a, void* hip_str
     q.dy = a->dh; q.lddy = a->lddh; q.gate = a->gate; q.up = a->up; q.ldg = a->ldg;
     q.rows = a->rows; q.cols = a->out; q.width = l.width;
     q.dz = b.slope ? ws : nullptr;
-    q.sums = a->db_gate ? (float*)(ws + l.sums) : nullptr;
+    q.rest = l.rest;
+    if (l.blocks > 1) {
+      q.sums = a->db_gate ? (float*)(ws + l.sums) : nullptr;
+    } else {
+      q.bias = a->db_gate;
+      q.bias2 = a->db_up;
+    }
+    q.bias_dtype = a->dbias_dtype;
     q.rows_per_block = l.rows_per_block; q.blocks = l.blocks; q.act = a->act;
     TA_TRY(hip_status(launch_slope(a->dtype, true, q, s), "gradients before the activation"));
   }
-  if (a->db_gate) {
+  if (a->db_gate && l.blocks != 1) {
     ColumnSums c{(const float*)(ws + l.sums), a->out, 2 * a->out, l.blocks, 2, a->dbias_dtype, {a->db_gate, a->db_up}};
     TA_TRY(hip_status(launch_column_sums(c, s), "gradients of the biases"));
   }

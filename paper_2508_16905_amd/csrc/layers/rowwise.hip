@@ -9,6 +9,19 @@ namespace {
 
 constexpr int kSlopeCols = 256, kSlopeLanes = kSlopeCols / 8, kSlopeRows = 256 / kSlopeLanes;
 
+template <int DT>
+__device__ __forceinline__ void store_parts(const SlopeArgs& a, int64_t at, float (&v)[8]) {
+  store8<DT>(a.dz, at, 8, v);
+  if (DT != kFP32 && a.rest) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float kept = (float)narrow<DT>(v[i]);
+      v[i] = __builtin_isfinite(kept) ? v[i] - kept : 0.0f;
+    }
+    store8<DT>(a.dz, at + a.rest, 8, v);
+  }
+}
+
 // dz = s drop(dy) act'(pre), or dg = dh up act'(gate) and du = dh act(gate); with the sums of a block of rows per column.
 // A workgroup has 256 columns, 32 lanes of eight, and eight rows at a time.
 template <int DT, bool GATED>
@@ -41,8 +54,8 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a, Drop drop) {
           sum[8 + i] += du[i];
         }
         if (a.dz) {
-          store8<DT>(a.dz, r * 2 * a.width + col, 8, d);
-          store8<DT>(a.dz, r * 2 * a.width + a.width + col, 8, du);
+          store_parts<DT>(a, r * 2 * a.width + col, d);
+          store_parts<DT>(a, r * 2 * a.width + a.width + col, du);
         }
       } else {
         scale_drop8(drop, key, (uint64_t)r * (uint64_t)a.cols + (uint64_t)col, d);
@@ -57,11 +70,11 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a, Drop drop) {
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += d[i];
-        if (a.dz) store8<DT>(a.dz, r * a.width + col, 8, d);
+        if (a.dz) store_parts<DT>(a, r * a.width + col, d);
       }
     }
   }
-  if (!a.sums) return;
+  if (!a.sums && !a.bias) return;
   __shared__ float part[kSlopeRows][kSlopeCols + 4];
 #pragma unroll
   for (int v = 0; v < kSums / 8; ++v) {
@@ -72,7 +85,10 @@ __global__ __launch_bounds__(256) void k_slope(SlopeArgs a, Drop drop) {
 #pragma unroll
     for (int r = 0; r < kSlopeRows; ++r) s += part[r][threadIdx.x];
     const int64_t c = (int64_t)blockIdx.x * kSlopeCols + threadIdx.x;
-    if (c < a.cols) as_global<float>(a.sums)[((int64_t)blockIdx.y * (kSums / 8) + v) * a.cols + c] = s;
+    if (c < a.cols) {
+      if (a.bias) store1_of(a.bias_dtype, v ? a.bias2 : a.bias, c, s);
+      else as_global<float>(a.sums)[((int64_t)blockIdx.y * (kSums / 8) + v) * a.cols + c] = s;
+    }
     __syncthreads();
   }
 }
