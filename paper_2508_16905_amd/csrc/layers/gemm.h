@@ -11,8 +11,9 @@
 // products the six largest are summed, those of one scale in one accumulator; what is dropped is at most 2^-26 of a product.
 // Six bf16 products have 2.6 times the rate of the fp32 matrix instructions (2.5 PFLOP/s / 6 = 417 and 157 TFLOP/s).
 //
-// Three forms.  Wide: a tile ahead in registers, fragments of the next 32 k ahead of these products, any strides and alignment
-// (fp32: the operands' parts, laid out by k_pack); the result has the size of a tile at least.  Staged: small tiles,
+// Four forms.  Direct: 16 bits, loads straight to a ring of tiles in LDS; every load has to be aligned to 16 bytes.  Wide: a
+// tile ahead in registers, fragments of the next 32 k ahead of these products, any strides and alignment (fp32: the operands'
+// parts, laid out by k_pack).  For both the result has the size of a tile at least.  Staged: small tiles,
 // fp32 split on the way; for small products, where KG groups of wavefronts share the k of one tile; no operand's rows are
 // shorter than eight.  Short: the same with operands loaded element by element, for those that have shorter rows.
 #pragma once
@@ -24,7 +25,7 @@ namespace triaccel {
 namespace layers {
 
 enum Layout : int { KC = 0, KS = 1 };
-enum Form : int { kStaged = 0, kWide = 1, kShort = 2 };
+enum Form : int { kStaged = 0, kWide = 1, kShort = 2, kDirect = 3 };
 enum Epi : int { kEpiLinear = 0, kEpiGated = 1, kEpiStore = 2 };
 
 struct GemmArgs {
@@ -70,56 +71,83 @@ __device__ __forceinline__ void epi_columns(const GemmArgs& g, int64_t col, Colu
     if (g.drop.limit) s.key = drop_key(g.drop);
   }
 }
-// v[n], v[n + 1], ... to the front
+// v[n], v[n + 1], ... to the front.  With masks: a choice between two elements would be made one of addresses, and the array be
+// searched element by element (6400 instructions a batch of rows; a last tile that begins earlier took 110 us longer).
 __device__ __forceinline__ void drop_first(float (&v)[8], int n) {
 #pragma unroll
-  for (int bit = 4; bit > 0; bit >>= 1)
+  for (int bit = 4; bit > 0; bit >>= 1) {
+    const uint32_t moved = n & bit ? ~0u : 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i + bit < 8) v[i] = n & bit ? v[i + bit] : v[i];
+      if (i + bit < 8) v[i] = u2f((f2u(v[i]) & ~moved) | (f2u(v[i + bit]) & moved));
+  }
 }
-// `count` of eight columns from `col` on (fewer where the row ends).
+// What a row's eight columns are added to.
 template <int DT, int EPI>
-__device__ __forceinline__ void epi_row(const GemmArgs& g, const ColumnState& s, int64_t row, int64_t col, int count, float (&v)[8], float (&u)[8]) {
+__device__ __forceinline__ Elem8<DT> epi_residual(const GemmArgs& g, int64_t row, int64_t col, int count) {
+  if (EPI != kEpiLinear || !g.residual) return Elem8<DT>{};
+  return load_raw8<DT>((const Elem<DT>*)g.residual + row * g.ldr + col, g.n - col < count ? g.n - col : count);
+}
+// `count` of eight columns from `col` on (fewer where the row ends) of N rows from `row` on, `step` apart, those that are `in`.
+// Several rows at a time, so that one's waits are filled by another's instructions.
+template <int DT, int EPI, int N>
+__device__ __forceinline__ void epi_rows(const GemmArgs& g, const ColumnState& s, int64_t row, int step, const bool (&in)[N], int64_t col, int count,
+                                         const Elem8<DT> (&residual)[N], float (&v)[N][8], float (&u)[N][8]) {
   const int64_t left = g.n - col < count ? g.n - col : count;
   constexpr bool kExact = DT == kFP32;
+#define TA_ROWS              \
+  _Pragma("unroll") for (int b = 0; b < N; ++b)
+#define TA_EACH              \
+  _Pragma("unroll") for (int b = 0; b < N; ++b) _Pragma("unroll") for (int i = 0; i < 8; ++i)
   if constexpr (EPI == kEpiStore) {
-    const bool second = row >= g.csplit;
-    if (!second && row >= g.crows) return;
-    void* c = second ? g.c2 : g.c;
-    const int64_t at = (second ? row - g.csplit : row) * g.ldc + col;
-    if (g.c_fp32) store8<kFP32>(c, at, left, v);
-    else store8<DT>(c, at, left, v);
+    TA_ROWS {
+      const int64_t at_row = row + b * step;
+      const bool second = at_row >= g.csplit;
+      if (!in[b] || (!second && at_row >= g.crows)) continue;
+      void* c = second ? g.c2 : g.c;
+      const int64_t at = (second ? at_row - g.csplit : at_row) * g.ldc + col;
+      if (g.c_fp32) store8<kFP32>(c, at, left, v[b]);
+      else store8<DT>(c, at, left, v[b]);
+    }
   } else if constexpr (EPI == kEpiGated) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] += s.bias[i];
-      u[i] += s.bias2[i];
+    TA_EACH {
+      v[b][i] += s.bias[i];
+      u[b][i] += s.bias2[i];
     }
     if (g.pre) {
-      store8<DT>(g.pre, row * g.ldpre + col, left, v);
-      store8<DT>(g.pre2, row * g.ldpre + col, left, u);
+      TA_ROWS if (in[b]) {
+        store8<DT>(g.pre, (row + b * step) * g.ldpre + col, left, v[b]);
+        store8<DT>(g.pre2, (row + b * step) * g.ldpre + col, left, u[b]);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = act_value<kExact>(g.act, v[i]) * u[i];
-    store8<DT>(g.c, row * g.ldc + col, left, v);
+    act_rows<kExact>(g.act, v);
+    TA_EACH v[b][i] *= u[b][i];
+    TA_ROWS if (in[b]) store8<DT>(g.c, (row + b * step) * g.ldc + col, left, v[b]);
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += s.bias[i];
-    if (g.pre) store8<DT>(g.pre, row * g.ldpre + col, left, v);
-    if (g.act != kNone) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = act_value<kExact>(g.act, v[i]);
+    TA_EACH v[b][i] += s.bias[i];
+    if (g.pre) {
+      TA_ROWS if (in[b]) store8<DT>(g.pre, (row + b * step) * g.ldpre + col, left, v[b]);
     }
-    scale_drop8(g.drop, s.key, (uint64_t)row * (uint32_t)g.n + (uint64_t)col, v);
+    act_rows<kExact>(g.act, v);
+    if (g.drop.limit) {
+      TA_ROWS drop8(g.drop, s.key, (uint64_t)(row + b * step) * (uint32_t)g.n + (uint64_t)col, v[b]);
+    } else {
+      TA_EACH v[b][i] *= g.drop.factor;
+    }
     if (g.residual) {
-      float r[8];
-      load8<DT>(g.residual, row * g.ldr + col, left, r);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += r[i];
+      TA_EACH v[b][i] += (float)residual[b][i];
     }
-    store8<DT>(g.c, row * g.ldc + col, left, v);
+    TA_ROWS if (in[b]) store8<DT>(g.c, (row + b * step) * g.ldc + col, left, v[b]);
   }
+#undef TA_EACH
+#undef TA_ROWS
+}
+// One row.
+template <int DT, int EPI>
+__device__ __forceinline__ void epi_row(const GemmArgs& g, const ColumnState& s, int64_t row, int64_t col, int count, float (&v)[1][8], float (&u)[1][8]) {
+  const bool in[1] = {true};
+  const Elem8<DT> residual[1] = {epi_residual<DT, EPI>(g, row, col, count)};
+  epi_rows<DT, EPI, 1>(g, s, row, 0, in, col, count, residual, v, u);
 }
 
 // ---- tiles in LDS ------------------------------------------------------------------------------------------------
@@ -178,7 +206,7 @@ __device__ __forceinline__ int on_xcd(int id, int total) {
 
 template <int DT_, int LA, int LB, int BM_, int BN_, int WR, int WC, int KG, int EPI_, int FORM, int AP = 1>
 struct Gemm {
-  static constexpr bool WIDE = FORM == kWide;
+  static constexpr bool DIRECT = FORM == kDirect, WIDE = FORM == kWide || DIRECT;
   static constexpr int DT = DT_, BM = BM_, BN = BN_, EPI = EPI_;
   // Parts of an operand in LDS.  AP = 2 (16 bits, staged): A comes in two parts, a value and what rounding took from it.
   static constexpr int kPlanes = DT == kFP32 ? 3 : 1, kPartsA = DT == kFP32 ? 3 : AP;
@@ -192,7 +220,8 @@ struct Gemm {
   static constexpr int kSlabCols = FN * 16, kSlabLd = kSlabCols + 4;
   static constexpr int kRound = FM < 4 ? FM : 4;          // fragments of rows that a wavefront's slab holds at a time
   static constexpr int kSlab = 16 * kRound * kSlabLd;     // floats of a wavefront
-  static constexpr int kTileBytes = KG * 2 * kTile * 2, kSlabBytes = WR * WC * kSlab * 4, kJoinBytes = (KG - 1) * BM * BN * 4;
+  static constexpr int kPart = BM * BK;                   // direct: elements of a place for one operand's tile, of five
+  static constexpr int kTileBytes = DIRECT ? 5 * kPart * 2 : KG * 2 * kTile * 2, kSlabBytes = WR * WC * kSlab * 4, kJoinBytes = (KG - 1) * BM * BN * 4;
   static constexpr int kMost = kSlabBytes > kJoinBytes ? kSlabBytes : kJoinBytes;
   static constexpr int kLdsBytes = kTileBytes > kMost ? kTileBytes : kMost;
   // columns of the result that a tile has
@@ -200,6 +229,7 @@ struct Gemm {
   static_assert(TA >= 1 && TB >= 1 && kAUnits % NT == 0 && kBUnits % NT == 0, "whole units per thread");
   static_assert(EPI != kEpiGated || FN % 2 == 0, "half of a wavefront's columns from each matrix");
   static_assert(!WIDE || KG == 1, "groups are for the staged form");
+  static_assert(!DIRECT || (DT != kFP32 && AP == 1 && BM == BN && FN % 4 == 0 && FM * FN / 4 % TA == 0), "tiles of the direct form");
   typedef typename std::conditional<WIDE, __bf16, Elem<DT>>::type E;  // WIDE: any 16 bits
   typedef f32x4 Acc[kPlanes][FM][FN];  // [q]: what counts 2^-8q
 
@@ -454,7 +484,22 @@ struct Gemm {
     if (over > 0) col += over;
     ColumnState state;
     if (!partial) epi_columns<EPI>(g, col, state);
-    static_assert(FM % kRound == 0, "whole rounds");
+    const int count = WIDE && over > 0 ? 8 - over : 8;
+    // Rows are worked on a few at a time, so that one's waits are filled by another's instructions (large tiles leave a SIMD one
+    // wavefront), and what they are added to is asked for a batch ahead (8192 x 10240 -> 4096 with dropout and residual, in
+    // bf16: 539 us one row at a time, 510 so).
+    constexpr int kTurns = 16 * kRound / kRows, kBatch = kTurns < 4 ? kTurns : 4;
+    static_assert(FM % kRound == 0 && 16 * kRound % kRows == 0 && kTurns % kBatch == 0, "whole rounds");
+    Elem8<DT> next[kBatch];
+    const auto ask = [&](int from, Elem8<DT> (&to)[kBatch]) {
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int row = row0 + (from + b) / kTurns * 16 * kRound + sub + (from + b) % kTurns * kRows;
+        to[b] = Elem8<DT>{};
+        if (mine && !partial && row < g.m && row >= tm * BM) to[b] = epi_residual<DT, EPI>(g, row, col, count);
+      }
+    };
+    ask(0, next);
 #pragma unroll
     for (int h = 0; h < FM; h += kRound) {
 #pragma unroll
@@ -463,30 +508,43 @@ struct Gemm {
         for (int j = 0; j < FN; ++j) *(f32x4*)(slab + (i * 16 + (lane & 15)) * kSlabLd + j * 16 + (lane >> 4) * 4) = acc[h + i][j];
       __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-      for (int r = sub; r < 16 * kRound; r += kRows) {
-        const int row = row0 + h * 16 + r;
-        if (mine && (partial || (row < g.m && row >= tm * BM))) {
-          const float* q = slab + r * kSlabLd + lane % kLanes * 8;
-          float v[8], u[8];
-          *(f32x4*)v = *(const f32x4*)q;
-          *(f32x4*)(v + 4) = *(const f32x4*)(q + 4);
+      for (int at = 0; at < kTurns; at += kBatch) {
+        Elem8<DT> now[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) now[b] = next[b];
+        const int after = (h / kRound) * kTurns + at + kBatch;
+        if (after < FM / kRound * kTurns) ask(after, next);
+        float v[kBatch][8], u[kBatch][8];
+        bool in[kBatch];
+        const int row = row0 + h * 16 + sub + at * kRows;
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          in[b] = mine && row + b * kRows < g.m && row + b * kRows >= tm * BM;
+          const float* q = slab + (sub < kRows ? sub + (at + b) * kRows : 0) * kSlabLd + lane % kLanes * 8;
+          *(f32x4*)v[b] = *(const f32x4*)q;
+          *(f32x4*)(v[b] + 4) = *(const f32x4*)(q + 4);
           if constexpr (EPI == kEpiGated) {
-            *(f32x4*)u = *(const f32x4*)(q + kOut);
-            *(f32x4*)(u + 4) = *(const f32x4*)(q + kOut + 4);
+            *(f32x4*)u[b] = *(const f32x4*)(q + kOut);
+            *(f32x4*)(u[b] + 4) = *(const f32x4*)(q + kOut + 4);
           }
-          if (partial) {
-            const int64_t base = (in_row + h * 16 + r) * BN + in_col;
-            store8<kFP32>(partial, base, 8, v);
-            if constexpr (EPI == kEpiGated) store8<kFP32>(partial, base + kCols, 8, u);
-          } else {
-            int count = 8;
-            if (WIDE && over > 0) {
-              count -= over;
-              drop_first(v, over);
-              if constexpr (EPI == kEpiGated) drop_first(u, over);
+        }
+        if (partial) {
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            const int64_t base = (in_row + h * 16 + sub + (at + b) * kRows) * BN + in_col;
+            if (!mine) continue;
+            store8<kFP32>(partial, base, 8, v[b]);
+            if constexpr (EPI == kEpiGated) store8<kFP32>(partial, base + kCols, 8, u[b]);
+          }
+        } else {
+          if (WIDE && over > 0) {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+              drop_first(v[b], over);
+              if constexpr (EPI == kEpiGated) drop_first(u[b], over);
             }
-            epi_row<DT, EPI>(g, state, row, col, count, v, u);
           }
+          epi_rows<DT, EPI, kBatch>(g, state, row, kRows, in, col, count, now, v, u);
         }
       }
       __builtin_amdgcn_wave_barrier();
@@ -653,6 +711,205 @@ struct Gemm {
     }
   }
 
+  // --- direct form ---
+  // The loads go to LDS without passing through registers, 16 bytes per lane, a wavefront's kilobyte in one run: the units of
+  // a row are exchanged (tile_unit) by what each lane asks for.  Written as assembly because the compiler, which does not know
+  // the ring, would wait for all loads before each read of LDS; they have no output registers, and the loop counts them.  (M0,
+  // which it sets, is read by nothing else here.)
+  typedef __attribute__((ext_vector_type(4))) uint32_t Resource;
+  static __device__ __forceinline__ void send(uint32_t to, uint32_t off, Resource from, uint32_t step) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(from), "s"(step) : "memory");
+  }
+  template <int N>
+  static __device__ __forceinline__ void arrived() {  // all loads but the last N
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+  }
+  // What lane `tid` asks for, from the tile's beginning, for even and odd t (the exchange of a KS tile's units changes every
+  // eighth k).
+  template <int L, int R, bool IS_B>
+  static __device__ __forceinline__ void direct_offsets(const GemmArgs& g, int tid, uint32_t (&off)[2]) {
+    const uint32_t ld = (uint32_t)(IS_B ? g.ldb : g.lda);
+#pragma unroll
+    for (int odd = 0; odd < 2; ++odd) {
+      if constexpr (L == KC) {
+        const uint32_t row = tid / (BK / 8), unit = tile_unit<KC, R, BK>(row, tid % (BK / 8)) % (BK / 8);
+        off[odd] = (row * ld + unit * 8) * 2u;
+      } else {
+        constexpr uint32_t kStep = NT / (R / 8);
+        const uint32_t k = tid / (R / 8), unit = tile_unit<KS, R, BK>(k + odd * kStep, tid % (R / 8)) % (R / 8);
+        off[odd] = (k * ld + unit * 8) * 2u;
+      }
+    }
+  }
+  // Where a tile of k of an operand begins.
+  template <int L, bool IS_B>
+  static __device__ __forceinline__ const E* part_base(const GemmArgs& g, const At& w, int r0, bool second) {
+    const int64_t ld = IS_B ? g.ldb : g.lda, koff = (IS_B ? 0 : (int64_t)w.seg * g.seg_step) + w.k0;
+    const E* p = (const E*)(IS_B ? (w.seg || second ? g.b2 : g.b) : g.a);
+    return p + (L == KC ? (int64_t)r0 * ld + koff : koff * ld + r0);
+  }
+  // Unit t NT + tid of a tile, for all lanes of a wavefront, to `to` (a byte address in LDS).
+  template <int L, int R, bool IS_B>
+  static __device__ __forceinline__ void send_part(const GemmArgs& g, Resource p, Resource p2, int t, const uint32_t (&off)[2], uint32_t to, int wave) {
+    constexpr int kStep = L == KC ? NT / (BK / 8) : NT / (R / 8);
+    static_assert(L == KC || kStep % 8 == 0, "two exchanges of units");
+    static_assert(L == KS || (kStep % 8 == 0 && FN * 8 % kStep == 0), "the rows of a load are of one matrix");
+    bool second = false;
+    const int step = IS_B && L == KC ? b_row(t * kStep, second) : t * kStep;
+    const uint32_t ld = (uint32_t)(IS_B ? g.ldb : g.lda);
+    send(to + (uint32_t)(t * NT + wave * 64) * 16u, off[t & 1], second ? p2 : p, (uint32_t)step * ld * 2u);
+  }
+
+  // Where a lane finds its part of a wavefront's F fragments (see `fragment`), made once: what differs between 32 k and the next,
+  // and between fragments of a KC tile, is the same for all lanes and part of the instruction.
+  template <int L, int F>
+  struct Reads {
+    static constexpr int kCount = L == KC ? 2 : F;
+    template <int R>
+    static __device__ __forceinline__ void begin(uint32_t (&at)[kCount], uint32_t base, int w, int lane) {
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) {
+        if constexpr (L == KC) {
+          at[i] = base + 16u * tile_unit<KC, R, BK>(w * F * 16 + (lane & 15), 4 * i + (lane >> 4));
+        } else {
+          const uint32_t k = 8 * (lane >> 4) + ((lane & 15) >> 2);
+          at[i] = base + 16u * tile_unit<KS, R, BK>(k, (uint32_t)(w * F * 2 + 2 * i) + ((lane >> 1) & 1)) + (lane & 1) * 8u;
+        }
+      }
+    }
+    template <int R>
+    static __device__ __forceinline__ s16x8 get(const uint32_t (&at)[kCount], uint32_t place, int i, int k0) {
+      if constexpr (L == KC) {
+        typedef __attribute__((address_space(3))) s16x8 Lds8;
+        return *(const Lds8*)(at[k0 / 32] + place + (uint32_t)i * 16u * BK * 2u);
+      } else {
+        typedef __attribute__((address_space(3))) s16x4 Lds4;
+        const uint32_t from = at[i] + place + (uint32_t)k0 * R * 2u;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4*)from);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4*)(from + 4u * R * 2u));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    }
+  };
+
+  // A ring of five places for one operand's tile of k each: A and B of two tiles, and one place more.  Part x (A of tile 0, B of
+  // tile 0, A of tile 1, ...) has place x % 5.  While tile kt is worked on, A of kt + 2 is sent for beside the products of its
+  // first 32 k and B of kt + 2 beside the second, into the places that the barrier before has freed; one barrier a tile.
+  // The fragments of the next 32 k are read beside the products of these.  Loads, reads and products are written in the order in
+  // which they are to be issued: a load for every eight products, since a CU takes in 64 bytes a cycle, half the time that
+  // the products take, and a wavefront whose load finds the queue full issues no products either (8192 x 4096 x 10240:
+  // evenly 488 us, all in a quarter of the time 600, eight in each 512 cycles 628).
+  // Whole tiles of k come first, those that pass the end of a segment last, through registers.
+  static __device__ __forceinline__ void direct_loop(const GemmArgs& g, Acc& acc, short* lds, int r0, int c0, int first, int last, int tid, int wave, int wm, int wn, int lane) {
+    const int per = g.seg / BK, whole = per * g.nseg;
+    const auto tile_at = [&](int kt) {
+      const int s = kt < whole ? (kt >= per ? 1 : 0) : kt - whole;
+      const int k0 = kt < whole ? (kt - s * per) * BK : per * BK;
+      return At{s, k0, g.seg - k0};
+    };
+    const int end = last < whole ? last : whole;
+    uint32_t off_a[2], off_b[2];
+    direct_offsets<LA, BM, false>(g, tid, off_a);
+    direct_offsets<LB, BN, true>(g, tid, off_b);
+    typedef __attribute__((address_space(3))) short Lds;
+    const uint32_t base = (uint32_t)(uintptr_t)(Lds*)lds;
+    constexpr int kGroups = FM * FN / 4, kEvery = kGroups / TA, kReads = FM + FN, kReadEach = 2 * kReads / kGroups;
+    constexpr uint32_t kPlaceBytes = kPart * 2;
+    const auto place = [](int x) { return x >= 5 ? x - 5 : x; };
+    const auto send_a = [&](Resource p, int slot, int t) { send_part<LA, BM, false>(g, p, p, t, off_a, base + (uint32_t)slot * kPlaceBytes, wave); };
+    const auto send_b = [&](Resource p, Resource p2, int slot, int t) { send_part<LB, BN, true>(g, p, p2, t, off_b, base + (uint32_t)slot * kPlaceBytes, wave); };
+    // tiles behind the last one: a resource of no bytes, from which nothing is loaded
+    const auto resource = [&](const E* p, int kt) {
+      const uint64_t v = (uint64_t)p;
+      return Resource{(uint32_t)v, (uint32_t)(v >> 32) & 0xffffu, kt < end ? 0x7fffffffu : 0u, (uint32_t)kBufferRaw};
+    };
+    const auto base_a = [&](int kt) { return resource(part_base<LA, false>(g, tile_at(kt), r0, false), kt); };
+    const auto base_b = [&](int kt, bool second) { return resource(part_base<LB, true>(g, tile_at(kt), c0, EPI == kEpiGated && second), kt); };
+    uint32_t at_a[Reads<LA, FM>::kCount], at_b[Reads<LB, FN>::kCount];
+    Reads<LA, FM>::template begin<BM>(at_a, base, wm, lane);
+    Reads<LB, FN>::template begin<BN>(at_b, base, wn, lane);
+    const auto read_one = [&](Frags& f, int slot_a, int slot_b, int k0, int x) {
+      if (x < FN) f.b[x][0] = Reads<LB, FN>::template get<BN>(at_b, (uint32_t)slot_b * kPlaceBytes, x, k0);
+      else f.a[x - FN][0] = Reads<LA, FM>::template get<BM>(at_a, (uint32_t)slot_a * kPlaceBytes, x - FN, k0);
+    };
+    const auto multiply4 = [&](const Frags& f, int q) {
+      const int i = q * 4 / FN, j0 = q * 4 % FN;
+#pragma unroll
+      for (int j = j0; j < j0 + 4; ++j) acc[0][i][j] = mfma<DT>(f.b[j][0], f.a[i][0], acc[0][i][j]);
+    };
+    const auto barrier = [&]() {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    int sa = 0;  // the place of A of tile kt
+    Frags f0, f1;
+    if (first < end) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const Resource pa = base_a(first + d), pb = base_b(first + d, false), pb2 = EPI == kEpiGated ? base_b(first + d, true) : pb;
+#pragma unroll
+        for (int t = 0; t < TA; ++t) send_a(pa, 2 * d, t);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) send_b(pb, pb2, 2 * d + 1, t);
+      }
+      arrived<TA + TB>();
+      barrier();
+#pragma unroll
+      for (int x = 0; x < kReads; ++x) read_one(f0, 0, 1, 0, x);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll 1
+      for (int kt = first; kt < end; ++kt) {
+        const int sb = place(sa + 1), na = place(sa + 2), nb = place(sa + 3);
+        const Resource pa = base_a(kt + 2);
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) {
+#pragma unroll
+          for (int x = q * kReadEach; x < (q + 1) * kReadEach; ++x)
+            if (x < kReads) read_one(f1, sa, sb, 32, x);
+          if (q % kEvery == 0) send_a(pa, place(sa + 4), q / kEvery);
+          __builtin_amdgcn_sched_barrier(0);
+          multiply4(f0, q);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        const Resource pb = base_b(kt + 2, false), pb2 = EPI == kEpiGated ? base_b(kt + 2, true) : pb;
+        arrived<TA>();  // tile kt + 1
+        barrier();
+#pragma unroll
+        for (int q = 0; q < kGroups; ++q) {
+#pragma unroll
+          for (int x = q * kReadEach; x < (q + 1) * kReadEach; ++x)
+            if (x < kReads) read_one(f0, na, nb, 0, x);
+          if (q % kEvery == 0) send_b(pb, pb2, sa, q / kEvery);
+          __builtin_amdgcn_sched_barrier(0);
+          multiply4(f1, q);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        sa = na;
+      }
+      arrived<0>();
+    }
+    for (int kt = first > whole ? first : whole; kt < last; ++kt) {
+      const At w = tile_at(kt);
+      s16x8 ra[TA], rb[TB];
+#pragma unroll
+      for (int t = 0; t < TA; ++t) ra[t] = get_edge<LA, BM, false>(g, w, r0, t, 0, tid);
+#pragma unroll
+      for (int t = 0; t < TB; ++t) rb[t] = get_edge<LB, BN, true>(g, w, c0, t, 0, tid);
+      meet();
+#pragma unroll
+      for (int t = 0; t < TA; ++t) put<LA, BM>(lds, t, 0, in_place<LA, BM>(g, w, ra[t], t, tid), tid);
+#pragma unroll
+      for (int t = 0; t < TB; ++t) put<LB, BN>(lds + kPart, t, 0, in_place<LB, BN>(g, w, rb[t], t, tid), tid);
+      meet();
+#pragma unroll 1
+      for (int k0 = 0; k0 < BK; k0 += 32) {
+        Frags f;
+        read(f, lds, k0, wm, wn, lane);
+        multiply<0, FM>(acc, f);
+      }
+    }
+  }
+
   // Group kg of KG has tiles first + kg, first + kg + KG, ...  What such a product waits for is memory, a round trip per tile:
   // kAhead tiles of a group are on their way to its registers.
   static constexpr int kAhead = 3;
@@ -728,7 +985,8 @@ struct Gemm {
     const int r0 = origin(tm * BM, g.m, BM), c0 = origin(tn * kCols, g.n, kCols);
     Acc acc;
     clear(acc);
-    if constexpr (WIDE) wide_loop(g, acc, lds, r0, c0, first, last, tid, wave, wm, wn, lane);
+    if constexpr (DIRECT) direct_loop(g, acc, lds, r0, c0, first, last, tid, wave, wm, wn, lane);
+    else if constexpr (WIDE) wide_loop(g, acc, lds, r0, c0, first, last, tid, wave, wm, wn, lane);
     else staged_loop(g, acc, lds, r0, c0, first, last, kg, tid, wm, wn, lane);
     __syncthreads();
     if constexpr (kPlanes == 3) {
@@ -764,7 +1022,7 @@ struct Gemm {
 };
 
 template <typename G>
-__global__ __launch_bounds__(G::kThreads) void k_gemm(GemmArgs g) {
+__global__ __launch_bounds__(G::kThreads, G::DIRECT && G::BM == 128 ? 2 : 1) void k_gemm(GemmArgs g) {
   __shared__ __attribute__((aligned(16))) short lds[G::kLdsBytes / 2];
   G::run(g, lds, (int)blockIdx.x);
 }
@@ -796,25 +1054,25 @@ __global__ __launch_bounds__(256) void k_join(GemmArgs g) {
   int64_t col = G::origin(tn * G::kCols, g.n, G::kCols) + in_col;
   const int over = (int)(tn * G::kCols - col);
   if (row >= g.m || row < tm * G::BM || col >= g.n || over >= 8) return;
-  float v[8] = {}, u[8] = {};
+  float v[1][8] = {}, u[1][8] = {};
   for (int s = 0; s < g.splits; ++s) {
     const float* p = g.partial + ((int64_t)tile * g.splits + s) * (G::BM * G::BN);
     float x[8];
     load8<kFP32>(p, in_row * G::BN + in_col, 8, x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += x[i];
+    for (int i = 0; i < 8; ++i) v[0][i] += x[i];
     if constexpr (G::EPI == kEpiGated) {
       load8<kFP32>(p, in_row * G::BN + G::kCols + in_col, 8, x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] += x[i];
+      for (int i = 0; i < 8; ++i) u[0][i] += x[i];
     }
   }
   int count = 8;
   if (over > 0) {
     col += over;
     count -= over;
-    drop_first(v, over);
-    if constexpr (G::EPI == kEpiGated) drop_first(u, over);
+    drop_first(v[0], over);
+    if constexpr (G::EPI == kEpiGated) drop_first(u[0], over);
   }
   ColumnState state;
   epi_columns<G::EPI>(g, col, state);

@@ -8,14 +8,21 @@
 namespace triaccel {
 namespace layers {
 
-template <typename G>
+// J: the instance that joins shares of k; it does not depend on the form.
+template <typename G, typename J = G>
 hipError_t launch_with(const GemmPlan& p, const GemmArgs& g, hipStream_t stream) {
   const int64_t rest = (int64_t)p.tiles_m * p.tiles_n - p.whole;
   k_gemm<G><<<dim3((uint32_t)(p.whole + rest * p.splits)), G::kThreads, 0, stream>>>(g);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || rest == 0) return e;
-  k_join<G><<<dim3((uint32_t)ceil_div(rest * (G::BM * G::kCols / 8), 256)), 256, 0, stream>>>(g);
+  k_join<J><<<dim3((uint32_t)ceil_div(rest * (G::BM * G::kCols / 8), 256)), 256, 0, stream>>>(g);
   return hipGetLastError();
+}
+
+// Whether every load of the direct form is aligned to 16 bytes: rows and where tiles begin in them.
+inline bool lies_aligned(int la, int lb, const GemmArgs& g) {
+  const auto bits = [](const void* p) { return (uint64_t)(uintptr_t)p; };
+  return ((bits(g.a) | bits(g.b) | bits(g.b2)) & 15u) == 0 && ((g.lda | g.ldb | g.seg_step) & 7) == 0 && (la == KC || g.m % 8 == 0) && (lb == KC || g.n % 8 == 0);
 }
 
 template <int DT, int LA, int LB, int EPI>
@@ -36,7 +43,18 @@ hipError_t launch_product(const GemmPlan& p, GemmArgs g, hipStream_t stream) {
     return launch_with<Gemm<DT, LA, LB, 32, 32, 2, 1, 1, EPI, kStaged>>(p, g, stream);
   }
   if constexpr (DT != kFP32) {
-    if (p.tile == kTileL) return launch_with<Gemm<DT, LA, LB, 256, 256, 2, 2, 1, EPI, kWide>>(p, g, stream);
+    typedef Gemm<DT, LA, LB, 256, 256, 2, 2, 1, EPI, kWide> L;
+    typedef Gemm<DT, LA, LB, 128, 128, 2, 2, 1, EPI, kWide> M;
+    if (lies_aligned(LA, LB, g)) {
+      // both operands by k: the addresses of the reads that turn leave too few registers (10928 x 2048, k = 4099: 246 us, wide 195)
+      if constexpr (LA == KC) {
+        if (p.tile == kTileL) return launch_with<Gemm<DT, LA, LB, 256, 256, 2, 2, 1, EPI, kDirect>, L>(p, g, stream);
+      } else if (p.tile == kTileL) {
+        return launch_with<L>(p, g, stream);
+      }
+      return launch_with<Gemm<DT, LA, LB, 128, 128, 2, 2, 1, EPI, kDirect>, M>(p, g, stream);
+    }
+    if (p.tile == kTileL) return launch_with<L>(p, g, stream);
   }
   return launch_with<Gemm<DT, LA, LB, 128, 128, 2, 2, 1, EPI, kWide>>(p, g, stream);
 }
@@ -80,7 +98,7 @@ hipError_t launch_thin(const GemmArgs& g, hipStream_t stream) {
   // a wavefront has two steps of 32 k at least, so that short k do not pay for sixteen wavefronts
   int waves = (g.seg + 63) / 64;
   waves = waves < 1 ? 1 : waves > kThinWaves ? kThinWaves : waves;
-  k_thin<DT, EPI><<<dim3((uint32_t)ceil_div(g.n, kThinCols)), waves * 64, 0, stream>>>(g);
+  k_thin<DT, EPI><<<dim3((uint32_t)ceil_div(g.n, kThinCols), (uint32_t)ceil_div(g.m, kThinRows)), waves * 64, 0, stream>>>(g);
   return hipGetLastError();
 }
 

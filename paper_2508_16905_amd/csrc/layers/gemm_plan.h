@@ -6,7 +6,7 @@ namespace triaccel {
 namespace layers {
 
 // X: 32 x 32, S: 64 x 64, both staged.  M: 128 x 128, L: 256 x 256, both in the wide form.
-// Short: as S, where an operand's rows are shorter than eight.  Thin: forward products of at most 16 rows (thin.h).
+// Short: as S, where an operand's rows are shorter than eight.  Thin: forward products of few rows (thin.h).
 enum Tile : int { kTileS = 0, kTileM = 1, kTileL = 2, kTileShort = 3, kTileThin = 4, kTileX = 5 };
 
 struct GemmPlan {
@@ -87,6 +87,12 @@ inline double pair_us(int tile, bool fp32, int parts, const GemmPlan& x, const G
   const double all = kb * (tx * x.per_split + tw * w.per_split) / 256.0, one = kb * (double)(x.per_split > w.per_split ? x.per_split : w.per_split);
   const double rounds = (tx + tw) / (fp32 || parts > 1 || tile == kTileS ? 256.0 : 512.0);
   return 4.0 + (rounds > 1.0 ? 2.5 * (rounds - 1.0) : 0.0) + (all > one ? all : one) / rate;
+}
+
+// Forward products in fp32, in workgroups of 16 rows and columns whose wavefronts share k.
+inline double thin_us(bool gated, int64_t m, int64_t n, int64_t k) {
+  const double kb = (double)((gated ? 48 : 32) * k * 4) / 1024.0;
+  return 4.0 + (double)ceil_div(ceil_div(m, 16) * ceil_div(n, 16), 256) * kb / 28.0;
 }
 
 // m x n results (gated: n columns of two products), k = nseg segments of seg.  `pack_us`: what it takes to lay the operands out

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../numerics.h"
 
 namespace triaccel {
@@ -176,6 +178,25 @@ __device__ __forceinline__ float act_value(int act, float z) {
     case kGelu: return z * normal_cdf(z);
     case kGeluTanh: return z * logistic<EXACT>(kTanhA * fmaf(kTanhB * z * z, z, z));
     default: return z;
+  }
+}
+// The same for N rows of eight, with one branch on the activation.
+template <bool EXACT, int N>
+__device__ __forceinline__ void act_rows(int act, float (&v)[N][8]) {
+  const auto all = [&](auto kind) {
+#pragma unroll
+    for (int b = 0; b < N; ++b) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[b][i] = act_value<EXACT>(decltype(kind)::value, v[b][i]);
+      if constexpr (decltype(kind)::value == kGelu) __builtin_amdgcn_sched_barrier(0);  // erfc: more rows at a time than registers
+    }
+  };
+  switch (act) {
+    case kRelu: all(std::integral_constant<int, kRelu>()); return;
+    case kSilu: all(std::integral_constant<int, kSilu>()); return;
+    case kGelu: all(std::integral_constant<int, kGelu>()); return;
+    case kGeluTanh: all(std::integral_constant<int, kGeluTanh>()); return;
+    default: return;
   }
 }
 // Past 32 the logistic function is 0 or 1 in fp32; held there, so that the cube cannot overflow in the slope.

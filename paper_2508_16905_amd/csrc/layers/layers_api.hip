@@ -173,9 +173,15 @@ ForwardPlan plan_forward(int32_t dtype, Product kind, int64_t rows, int64_t in, 
   if (two) f.q.op[2] = Operand{w2, ldw, out, in};
   f.q.op[3] = Operand{x, ldx, rows, in};
   unsigned need = two ? 14u : 10u;
-  // up to 16 rows: bound by reading the weights (10240 -> 4096 in bf16, one row: 18 us and a second launch of 4 in small tiles)
-  if (rows <= 16) f.g.tile = kTileThin;
-  else f.g = plan_gemm(dtype == TRIACCEL_FP32, two, pack_us(f.q, need), in, rows, out, in, 1);
+  // Small layers in fp32: 96 x 784 -> 128 10.3 us in tiles of 32 x 32, 6.1 so, 96 x 512 -> 512 7.2 and 5.0; in 16 bits, where
+  // nothing is split on the way, 4.9 and 4.0, but 64 x 4096 -> 1024 8.7 and 10.1: these stay in tiles.
+  // Up to 16 rows: bound by reading the weights (10240 -> 4096 in bf16, one row: 18 us and a second launch of 4 in small tiles)
+  const bool fp32 = dtype == TRIACCEL_FP32;
+  if (rows > 16) f.g = plan_gemm(fp32, two, pack_us(f.q, need), in, rows, out, in, 1);
+  if (rows <= 16 || (fp32 && rows <= 4096 && thin_us(two, rows, out, in) < f.g.us)) {
+    f.g = GemmPlan{};
+    f.g.tile = kTileThin;
+  }
   if (!is_wide(f.g)) need = 0;
   lay_out(f.q, 0, need, f.g.partial_bytes);
   return f;

@@ -1,6 +1,6 @@
-// Products of few rows (at most 16): y = act(x W^T + b) ... and the gated pair, for single tokens.
+// Products of few rows, y = act(x W^T + b) ... and the gated pair: single tokens and small layers.
 //
-// Bound by reading the weights once.  A workgroup has 16 columns of the result (16 rows of W, of both matrices if gated) and
+// Up to 16 rows they are bound by reading the weights once; small layers by the time that one tile takes.  A workgroup has 16 rows and columns of the result (16 rows of W, of both matrices if gated) and
 // its wavefronts deal the k among themselves, 32 at a time: no LDS on the way, eight loads of W in flight per lane, the matrix
 // cores for the products (their rate does not matter, but one instruction takes 512 products' worth of work off the vector
 // ALUs), and one sum over the wavefronts at the end.
@@ -38,9 +38,9 @@ struct Thin {
     constexpr int kAhead = DT == kFP32 ? 2 : 4;  // steps of 32 k whose loads are in flight
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int waves = (int)blockDim.x >> 6;
-    const int c0 = (int)blockIdx.x * kThinCols;
+    const int c0 = (int)blockIdx.x * kThinCols, r0 = (int)blockIdx.y * kThinRows;
     // rows that do not exist are read as the last one and not written
-    const int col = c0 + (lane & 15) < g.n ? c0 + (lane & 15) : g.n - 1, row = (lane & 15) < g.m ? lane & 15 : g.m - 1;
+    const int col = c0 + (lane & 15) < g.n ? c0 + (lane & 15) : g.n - 1, row = r0 + (lane & 15) < g.m ? r0 + (lane & 15) : g.m - 1;
     const int in = (lane >> 4) * 8;
     const E* w[kMats];
     w[0] = (const E*)g.b + (int64_t)col * g.ldb + in;
@@ -94,14 +94,14 @@ struct Thin {
       *(f32x4*)&part[wave][i][lane & 15][(lane >> 4) * 4] = acc[i][0];
     }
     __syncthreads();
-    const int out_row = (int)threadIdx.x >> 1, out_col = ((int)threadIdx.x & 1) * 8;
-    if (out_row >= g.m || out_row >= kThinRows || c0 + out_col >= g.n) return;
-    float v[8] = {}, u[8] = {};
+    const int in_row = (int)threadIdx.x >> 1, out_row = r0 + in_row, out_col = ((int)threadIdx.x & 1) * 8;
+    if (out_row >= g.m || in_row >= kThinRows || c0 + out_col >= g.n) return;
+    float v[1][8] = {}, u[1][8] = {};
     for (int q = 0; q < waves; ++q) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        v[i] += part[q][0][out_row][out_col + i];
-        if constexpr (kMats == 2) u[i] += part[q][1][out_row][out_col + i];
+        v[0][i] += part[q][0][in_row][out_col + i];
+        if constexpr (kMats == 2) u[0][i] += part[q][1][in_row][out_col + i];
       }
     }
     ColumnState state;
