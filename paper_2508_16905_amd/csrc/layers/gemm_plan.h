@@ -35,8 +35,8 @@ inline GemmPlan plan_tile(int tile, bool fp32, bool gated, int64_t m, int64_t n,
   const int64_t k_tiles = seg > 0 ? ceil_div(seg, bk) * nseg : 1, all = (int64_t)p.tiles_m * p.tiles_n;
   p.groups = !wide && tile != kTileShort && k_tiles >= 4 && all <= 1024 ? (fp32 && tile == kTileS ? 2 : 4) : 1;
   const int64_t slots = tile == kTileL ? 256 : tile == kTileM ? (fp32 ? 256 : 512) : 256;
-  const double join = 6.5, fixed = wide ? 5.0 : 4.0;
-  const double per_k = tile == kTileL ? 1.75 : fp32 ? 1.85 : all > 256 ? 1.45 : 1.0;
+  const double join = 6.5, fixed = !wide ? 4.0 : tile == kTileL ? 12.0 : 5.0;
+  const double per_k = tile == kTileL ? 1.5 : fp32 ? 1.85 : all > 256 ? 1.32 : 0.8;
   const double kb = (double)(2 * edge * bk * (fp32 ? 4 : 2)) / 1024.0;
   // `work` workgroups of `k` tiles of k each
   const auto time = [&](int64_t work, int64_t k) {

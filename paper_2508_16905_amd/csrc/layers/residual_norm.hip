@@ -154,9 +154,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void k_residual_norm(NormArgs a)
 // long as the reading and writing): the next row is loaded before this one is worked on, the vectors stay in
 // LDS (V = 1; in registers they would leave room for half as many wavefronts), and rows that fill their lanes (FULL) go without
 // a test per element.
-template <int DT, int T, int V, bool FULL>
+template <int DT, int T, int V, bool FULL, bool CENTRED>
 __global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual_norm_grad(NormGradArgs a) {
-  constexpr bool kKeep = V == 1;
+  constexpr bool kKeep = V == 1, kAhead = V == 1;
   __shared__ float lds[2 * 2 * (T / 64)];
   __shared__ f32x4 kept[kKeep ? 8 * T : 1];  // a lane reads only what it wrote
   const int lane = threadIdx.x;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual
   const int64_t r0 = team * a.rows_per_team, r1 = r0 + a.rows_per_team < a.rows ? r0 + a.rows_per_team : a.rows;
   int turn = 0;
   const float cols = (float)a.cols, inv = 1.0f / cols;
-  const bool next = a.norm.kind && a.dy, post = a.b && a.post.kind, next_centred = a.norm.kind == 2, post_centred = a.post.kind == 2;
+  const bool next = a.norm.kind && a.dy, post = a.b && a.post.kind, next_centred = CENTRED && a.norm.kind == 2, post_centred = CENTRED && a.post.kind == 2;
   int col[V], left[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
@@ -250,7 +250,7 @@ __global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual
       q_b[v] = get(a.b, a.ldb);
     }
   };
-  fetch(r0);
+  if (kAhead) fetch(r0);
   for (int64_t row = r0; row < r1; ++row) {
     if (row == group_end) {
       if (a.dgate) flush_gate();
@@ -258,6 +258,7 @@ __global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual
       group_end += a.rows_per_gate;
       keep_gate();
     }
+    if (!kAhead) fetch(row);
     float d[V][8], r[V][8], dy[V][8], b[V][8];
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual
         r[v][i] = (float)q_r[v][i];
         b[v][i] = (float)q_b[v][i];
       }
-    if (row + 1 < r1) fetch(row + 1);
+    if (kAhead && row + 1 < r1) fetch(row + 1);
     // both rows' statistics: means, then sums of squares around them
     float rstd = 0.0f, brstd = 1.0f;
     {
@@ -310,7 +311,7 @@ __global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual
         for (int i = 0; i < 8; ++i) {
           r[v][i] *= rstd;
           nw[v][i] = fmaf(dy[v][i], r[v][i], nw[v][i]);
-          nb[v][i] += dy[v][i];
+          if (CENTRED) nb[v][i] += dy[v][i];
           dy[v][i] *= w[i];
           s[0] = fmaf(dy[v][i], r[v][i], s[0]);
           s[1] += dy[v][i];
@@ -350,7 +351,7 @@ __global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual
           // past the end the factor is 0, whatever d became there
           const float dp = g[i] * d[v][i];
           pw[v][i] = fmaf(dp, b[v][i], pw[v][i]);
-          pb[v][i] += dp;
+          if (CENTRED) pb[v][i] += dp;
           d[v][i] = dp * w[i];
           s[0] = fmaf(d[v][i], b[v][i], s[0]);
           s[1] += d[v][i];
@@ -386,9 +387,9 @@ __global__ __launch_bounds__(T, T >= 512 || DT != kFP32 ? 4 : 3) void k_residual
   for (int v = 0; v < V; ++v) {
     const int64_t at = team * kNormVectors * a.cols + col[v];
     if (a.dnw) store8<kFP32>(a.sums, at, left[v], nw[v]);
-    if (a.dnb) store8<kFP32>(a.sums, at + a.cols, left[v], nb[v]);
+    if (CENTRED && a.dnb) store8<kFP32>(a.sums, at + a.cols, left[v], nb[v]);
     if (a.dpw) store8<kFP32>(a.sums, at + 2 * a.cols, left[v], pw[v]);
-    if (a.dpb) store8<kFP32>(a.sums, at + 3 * a.cols, left[v], pb[v]);
+    if (CENTRED && a.dpb) store8<kFP32>(a.sums, at + 3 * a.cols, left[v], pb[v]);
     if (a.dgate && !a.rows_per_gate) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) gs[v][i] *= a.scale;
@@ -458,8 +459,12 @@ hipError_t forward(const NormArgs& a, hipStream_t stream) {
 }
 template <int DT, int T, int V>
 void backward_of(const NormGradArgs& a, hipStream_t stream) {
-  if (a.cols == T * V * 8) k_residual_norm_grad<DT, T, V, true><<<dim3((uint32_t)a.teams), T, 0, stream>>>(a);
-  else k_residual_norm_grad<DT, T, V, false><<<dim3((uint32_t)a.teams), T, 0, stream>>>(a);
+  const bool full = a.cols == T * V * 8, centred = a.norm.kind == 2 || a.post.kind == 2 || a.dnb || a.dpb;
+  const dim3 grid((uint32_t)a.teams);
+  if (full && centred) k_residual_norm_grad<DT, T, V, true, true><<<grid, T, 0, stream>>>(a);
+  else if (full) k_residual_norm_grad<DT, T, V, true, false><<<grid, T, 0, stream>>>(a);
+  else if (centred) k_residual_norm_grad<DT, T, V, false, true><<<grid, T, 0, stream>>>(a);
+  else k_residual_norm_grad<DT, T, V, false, false><<<grid, T, 0, stream>>>(a);
 }
 template <int DT>
 hipError_t backward(const NormGradArgs& a, hipStream_t stream) {
