@@ -137,7 +137,8 @@ double pack_us(const Products& q, unsigned need) {
   uint64_t bytes = 0;
   for (int i = 0; i < 4; ++i) {
     if (!(need >> i & 1u)) continue;
-    if (q.op[i].cols >= (1 << 21) || q.op[i].ld >= (1 << 21) || q.op[i].rows * q.op[i].cols >= (int64_t)1 << 32) return 1e30;
+    if (q.op[i].cols >= (1 << 21) || q.op[i].ld >= (1 << 21)) return 1e30;
+    if (q.dtype == TRIACCEL_FP32 && q.op[i].rows * q.op[i].cols >= (int64_t)1 << 32) return 1e30;
     bytes += packed_bytes(q.op[i]) / 6 * 10;
   }
   return q.dtype == TRIACCEL_FP32 && bytes ? 5.0 + (double)bytes / 4.0e6 : 0.0;
@@ -374,7 +375,7 @@ int check_norm(const triaccel_norm_spec& n, const char* name) {
 }
 NormSide side_of(const triaccel_norm_spec& n) { return NormSide{n.weight, n.bias, n.kind, n.dtype, n.eps}; }
 int check_gate(const void* gate, int64_t ld, int64_t rows_per_gate, int64_t cols, int32_t dtype) {
-  if (rows_per_gate < 0) return refuse(TRIACCEL_E_INVALID_ARG, "rows_per_gate is below 0");
+  if (rows_per_gate < 0 || rows_per_gate > kMaxDim) return refuse(TRIACCEL_E_INVALID_ARG, "rows_per_gate is below 0, or too large");
   TA_TRY(check_vector(gate, dtype, "gate"));
   if (gate && rows_per_gate > 0) return check_matrix(gate, ld, 1, cols, dtype, "gate");
   return TRIACCEL_OK;
@@ -384,7 +385,7 @@ int check_norm_backward(const triaccel_residual_norm_backward_args* a) {
   if (a->struct_size != sizeof(*a)) return refuse(TRIACCEL_E_INVALID_ARG, "struct_size");
   TA_TRY(check_sizes(a->dtype, a->rows, a->cols, 1));
   if (a->cols > TRIACCEL_NORM_MAX_COLS) return refuse(TRIACCEL_E_INVALID_ARG, "cols: above TRIACCEL_NORM_MAX_COLS");
-  if (a->rows_per_gate < 0) return refuse(TRIACCEL_E_INVALID_ARG, "rows_per_gate is below 0");
+  if (a->rows_per_gate < 0 || a->rows_per_gate > kMaxDim) return refuse(TRIACCEL_E_INVALID_ARG, "rows_per_gate is below 0, or too large");
   return TRIACCEL_OK;
 }
 struct NormLayout {
@@ -636,7 +637,8 @@ int triaccel_dropout(const triaccel_dropout_args* a, void* hip_stream) {
   TA_TRY(check_matrix(a->x, a->ldx, a->rows, a->cols, a->dtype, "x"));
   if (a->residual) TA_TRY(check_matrix(a->residual, a->ldr, a->rows, a->cols, a->dtype, "residual"));
   TA_TRY(check_matrix(a->y, a->ldy, a->rows, a->cols, a->dtype, "y"));
-  if (a->rows * ceil_div(a->cols, 512) > (int64_t)1 << 25) return refuse(TRIACCEL_E_INVALID_ARG, "dropout: more than 2^25 rows of 512 columns");
+  const bool dense = a->ldx == a->cols && a->ldy == a->cols && (!a->residual || a->ldr == a->cols);  // worked on as one long row
+  if ((dense ? ceil_div(a->rows * a->cols, 512) : a->rows * ceil_div(a->cols, 512)) > (int64_t)1 << 25) return refuse(TRIACCEL_E_INVALID_ARG, "dropout: more than 2^25 rows of 512 columns");
   if (a->rows == 0) return TRIACCEL_OK;
   const DropoutArgs d{a->rows, a->cols, a->x, a->residual, a->ldx, a->ldr, a->ldy, a->y};
   return hip_status(launch_dropout(a->dtype, d, drop_of(a->drop, a->scale), (hipStream_t)hip_stream), "dropout");

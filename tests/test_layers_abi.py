@@ -139,3 +139,17 @@ def test_workspaces_grow_with_what_they_hold(lib):
 def test_the_wrapper_refuses_tensors_of_the_host():
     with pytest.raises(ValueError):
         ta.linear(torch.ones(2, 4), torch.ones(3, 4))
+
+
+@pytest.mark.parametrize("rows_per_gate", [1 << 31, 1 << 62, -(1 << 62)])
+def test_groups_of_rows_past_the_sizes_are_refused(lib, rows_per_gate):
+    assert lib.triaccel_residual_norm(C.byref(norm(gate=ADDRESS, gate_dtype=B.FP32, ldgate=16, rows_per_gate=rows_per_gate)), None) == -1
+    a = B.ResidualNormBackwardArgs(struct_size=C.sizeof(B.ResidualNormBackwardArgs), dtype=B.BF16, rows=4, cols=16, residual=ADDRESS, ldr=16, dvec_dtype=2,
+                                   scale=1.0, rows_per_gate=rows_per_gate)
+    assert lib.triaccel_residual_norm_backward_workspace(C.byref(a)) == -1
+
+
+def test_dropout_of_more_rows_than_a_launch_has(lib):
+    d = B.DropoutArgs(struct_size=C.sizeof(B.DropoutArgs), dtype=B.BF16, rows=(1 << 25) + 1, cols=16, x=ADDRESS, ldx=24, y=ADDRESS, ldy=16, scale=1.0,
+                      drop=B.DropoutSpec(0.5, 1, 2, None))
+    assert lib.triaccel_dropout(C.byref(d), None) == -1
