@@ -81,7 +81,8 @@ typedef struct {
 int64_t triaccel_linear_workspace(const triaccel_linear_args *args);
 int triaccel_linear(const triaccel_linear_args *args, void *hip_stream);
 
-/* dz = s drop(dy) act'(pre), dx = dz W, dW = dz^T x, db = sum over the rows of dz; the gradient of the residual is dy. */
+/* dz = s drop(dy) act'(pre), dx = dz W, dW = dz^T x, db = sum over the rows of dz; the gradient of the residual is dy.
+   dz is in fp32 for db and, in large layers, rounded to `dtype` for the products (likewise dg and du of the gated block). */
 typedef struct {
   uint32_t struct_size; /* sizeof(triaccel_linear_backward_args) */
   int32_t dtype;
