@@ -1027,17 +1027,20 @@ __global__ __launch_bounds__(G::kThreads, G::DIRECT && G::BM == 128 ? 2 : 1) voi
   G::run(g, lds, (int)blockIdx.x);
 }
 
-// Two products in one launch, for the gradients of a small layer: the first workgroups have the one, the others the other.
+// Two products in one launch, for both gradients of a layer: the first workgroups have the one, the others the other.
 struct PairArgs {
   GemmArgs x, w;
-  int32_t first;  // workgroups of x
+  int32_t first;    // workgroups of the first
+  int32_t w_first;  // which that is
 };
 template <typename GX, typename GW>
 __global__ __launch_bounds__(GX::kThreads) void k_pair(PairArgs p) {
   static_assert(GX::kThreads == GW::kThreads, "one workgroup size");
   __shared__ __attribute__((aligned(16))) short lds[(GX::kLdsBytes > GW::kLdsBytes ? GX::kLdsBytes : GW::kLdsBytes) / 2];
-  if ((int)blockIdx.x < p.first) GX::run(p.x, lds, (int)blockIdx.x);
-  else GW::run(p.w, lds, (int)blockIdx.x - p.first);
+  const bool second = (int)blockIdx.x >= p.first;
+  const int block = second ? (int)blockIdx.x - p.first : (int)blockIdx.x;
+  if (second == (p.w_first != 0)) GX::run(p.x, lds, block);
+  else GW::run(p.w, lds, block);
 }
 
 // The tiles of the result whose k was shared: eight columns of a row per thread, the shares in order, then the epilogue.

@@ -62,7 +62,9 @@ hipError_t launch_product(const GemmPlan& p, GemmArgs g, hipStream_t stream) {
 // The gradients of the input and of the weights in one launch; AP: parts of dz.
 template <int DT, int AP>
 hipError_t launch_both(const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x, const GemmArgs& w, hipStream_t stream) {
-  PairArgs p{x, w, px.tiles_m * px.tiles_n};
+  // the longer tiles first, so that the shorter ones fill the end
+  const bool w_first = pw.per_split > px.per_split;
+  PairArgs p{x, w, w_first ? pw.tiles_m * pw.tiles_n : px.tiles_m * px.tiles_n, w_first};
   const auto fill = [](GemmArgs& g, const GemmPlan& q) {
     g.tiles_m = q.tiles_m;
     g.tiles_n = q.tiles_n;
@@ -73,6 +75,16 @@ hipError_t launch_both(const GemmPlan& px, const GemmPlan& pw, const GemmArgs& x
   fill(p.x, px);
   fill(p.w, pw);
   const dim3 grid((uint32_t)(p.x.whole + p.w.whole));
+  if constexpr (DT != kFP32 && AP == 1) {
+    if (px.tile == kTileL) {
+      typedef Gemm<DT, KS, KS, 256, 256, 2, 2, 1, kEpiStore, kWide> GW;
+      typedef Gemm<DT, KC, KS, 256, 256, 2, 2, 1, kEpiStore, kDirect> GX;
+      typedef Gemm<DT, KC, KS, 256, 256, 2, 2, 1, kEpiStore, kWide> GU;
+      if (lies_aligned(KC, KS, x)) k_pair<GX, GW><<<grid, GX::kThreads, 0, stream>>>(p);
+      else k_pair<GU, GW><<<grid, GU::kThreads, 0, stream>>>(p);
+      return hipGetLastError();
+    }
+  }
   if (px.tile == kTileX) {
     typedef Gemm<DT, KC, KS, 32, 32, 2, 1, 4, kEpiStore, kStaged, AP> GX;
     typedef Gemm<DT, KS, KS, 32, 32, 2, 1, 4, kEpiStore, kStaged, AP> GW;

@@ -95,6 +95,16 @@ inline double thin_us(bool gated, int64_t m, int64_t n, int64_t k) {
   return 4.0 + (double)ceil_div(ceil_div(m, 16) * ceil_div(n, 16), 256) * kb / 28.0;
 }
 
+// Two products in 16 bits in one launch, in tiles of 256 x 256: what is left over after whole rounds of the one is filled by the
+// other.  All their work over the CUs, and half of a shorter tile at the end, where fewer and fewer are left.
+inline double large_pair_us(const GemmPlan& x, const GemmPlan& w) {
+  const double one_x = 1.5 * (double)x.per_split + 12.0, one_w = 1.6 * (double)w.per_split + 12.0;
+  const double tx = (double)x.tiles_m * x.tiles_n, tw = (double)w.tiles_m * w.tiles_n;
+  const double shorter = one_x < one_w ? one_x : one_w;
+  const double all = (tx * one_x + tw * one_w) / 256.0 + 0.5 * shorter, longest = one_x > one_w ? one_x : one_w;
+  return all > longest ? all : longest;
+}
+
 // m x n results (gated: n columns of two products), k = nseg segments of seg.  `pack_us`: what it takes to lay the operands out
 // for the wide form.
 // `shortest`: the shortest row of an operand.

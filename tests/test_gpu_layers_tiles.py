@@ -42,7 +42,7 @@ def test_alignment(shift, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("m,n,k", [(4099, 2056, 200), (520, 392, 264), (2050, 5464, 72), (1025, 1001, 136)])
+@pytest.mark.parametrize("m,n,k", [(4099, 2056, 200), (520, 392, 264), (2050, 5464, 72), (1025, 1001, 136), (4099, 5464, 1032), (1500, 2731, 521), (520, 4104, 2056)])
 def test_gated(m, n, k, dtype):
     g = generator("gated tiles", m, n, k, dtype)
     x, wg, wu = make(g, m, k, dtype), make(g, n, k, dtype, scale=k ** -0.5), make(g, n, k, dtype, scale=k ** -0.5)
